@@ -59,7 +59,7 @@ typedef enum {
 typedef enum { RGNN_F32 = 0, RGNN_BF16 = 1 } rgnn_dtype_t;
 enum { RGNN_LAYER_RGCN = 0, RGNN_LAYER_RGAT = 1, RGNN_LAYER_HGT = 2 };
 enum { RGNN_NORM_NONE = 0, RGNN_NORM_IN_DEGREE_PER_REL = 1 };
-enum { RGNN_ACT_NONE = 0, RGNN_ACT_RELU = 1 };
+enum { RGNN_ACT_NONE = 0, RGNN_ACT_RELU = 1, RGNN_ACT_SILU = 2 };
 enum { RGNN_MEM_HOST = 0, RGNN_MEM_DEVICE = 1 };
 enum { RGNN_COO = 0, RGNN_CSR_DST = 1 };
 
@@ -341,6 +341,80 @@ rgnn_status_t rgnn_hgt_bwd(const rgnn_graph_t* g, const rgnn_layer_desc_t* desc,
                            const void* mu, const void* out, const void* saved, const void* dOut, void* dX,
                            void* dWk, void* dWq, void* dWv, void* dWo, void* dWatt, void* dWmsg, void* dmu,
                            void* workspace, void* stream);
+
+/*
+ * Operators on the rows of all nodes, for what stands between the layers of a model and in its training step.  They
+ * need no graph.  Streams, workspaces, alignment and errors as for the layer calls; a call with no rows enqueues
+ * nothing but the zeros of its parameter gradients, and its row tensors may be NULL.
+ *
+ * Unlike the layers, whose results are fp32 whatever they read, these write the type they name: rows of 2 bytes pass
+ * from one operator, or layer, to the next without a conversion.  Sums and products are fp32 in every case, and a
+ * result is rounded once, to nearest even, where it is stored.
+ */
+
+/* Residual addition and root-mean-square norm, row by row:
+ *   sum = x + residual;   out = sum / sqrt(mean(sum^2) + eps) * weight
+ * x_dtype: x, dX.  sum_dtype: residual, sum, dSum, dResidual.  out_dtype: out, dOut.  RGNN_F32 or RGNN_BF16 each: a layer's
+ * fp32 rows can be added to a bf16 stream, an fp32 stream be handed to the next layer in bf16.  weight and dWeight are
+ * fp32.  The mean of the squares has to be in the range of fp32.
+ *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: dX, dResidual and dWeight are added to) */
+typedef struct {
+    int64_t rows;
+    int32_t width;               /* 1 .. 8192 */
+    int32_t x_dtype, sum_dtype, out_dtype;
+    float eps;                   /* finite, >= 0 */
+    uint32_t flags;
+} rgnn_norm_desc_t;
+rgnn_status_t rgnn_norm_workspace_bytes(const rgnn_norm_desc_t* desc, size_t* bwd_workspace);
+/* residual [rows, width] or NULL (nothing is added).  sum [rows, width], or NULL where it is not wanted.  out [rows, width].
+ * `out` is formed from the sum before that is rounded.  sum and out may each be x's or residual's own buffer (of the same
+ * type); other overlaps are not allowed. */
+rgnn_status_t rgnn_norm_fwd(const rgnn_norm_desc_t* desc, const void* x, const void* residual, const float* weight, void* sum,
+                            void* out, void* stream);
+/* sum: the forward's sum as stored (without a residual: x, with sum_dtype = x_dtype).  dOut: gradient of out; dSum: gradient that
+ * reaches sum on its other way, or NULL.  The gradients of x and of residual are the same numbers: dX and dResidual are
+ * written in their types, either may be NULL, and each may be dOut's or dSum's own buffer (of the same type).
+ * dWeight [width] or NULL. */
+rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const float* weight, const void* dOut, const void* dSum,
+                            void* dX, void* dResidual, float* dWeight, void* workspace, void* stream);
+
+/* Gated feed-forward block, row by row, with no tensor of the hidden width in memory:
+ *   out = (act(X Wg) * (X Wu)) Wd
+ * X, out [rows, width]; Wg, Wu [width, hidden]; Wd [hidden, width]; every tensor, gradients too, of type dtype.
+ *   activation RGNN_ACT_SILU (g / (1 + exp(-g))) or RGNN_ACT_RELU (its derivative at 0 is 0)
+ *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: every gradient is added to)
+ * RGNN_F32: products are formed from three bfloat16 planes per operand on the matrix cores, as close to 64 bits as fp32
+ * products are; operands below 2^-110 lose their last bits.  RGNN_BF16: act(g) u and the gradients of g and u are rounded
+ * to bfloat16 where they enter the next product.  An infinite or NaN entry, or a product that leaves the range of fp32, makes its row
+ * of out (dX), and the weights' gradients, NaN or infinite; the other rows are not touched by it. */
+typedef struct {
+    int64_t rows;
+    int32_t dtype;
+    int32_t width;               /* 32, 64 or 128 */
+    int32_t hidden;              /* 1 .. 16384 */
+    int32_t activation;
+    uint32_t flags;
+} rgnn_ffn_desc_t;
+rgnn_status_t rgnn_ffn_workspace_bytes(const rgnn_ffn_desc_t* desc, size_t* fwd_workspace, size_t* bwd_workspace);
+/* out may not share memory with an input. */
+rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, void* out,
+                           void* workspace, void* stream);
+/* dOut: gradient of out.  dX may be NULL; dWg, dWu, dWd are either all given or all NULL.  The hidden values are formed again:
+ * the forward keeps nothing. */
+rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
+                           void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream);
+
+/* Global norm of a model's gradients and clipping by it:
+ *   norm = sqrt(sum over all tensors of the sum of g^2);   clipped = g * min(1, max_norm / (norm + 1e-6))
+ * count tensors: HOST arrays of device pointers, element counts and types (RGNN_F32 or RGNN_BF16, mixed as they come), read before
+ * the call returns.  A pointer needs its element's alignment only; one of an empty tensor may be NULL.  norm: one float on the device.
+ * clipped == NULL: the norm alone (max_norm is ignored).  clipped[i] is grads[i] itself (in place) or memory that overlaps nothing
+ * else; EINVAL otherwise, also for a tensor that is clipped in place and given twice.
+ * Squares and sums are fp64, in a fixed order.  A NaN among the gradients makes the norm and all of `clipped` NaN; an infinite norm makes
+ * the finite ones 0; with max_norm = INFINITY nothing is clipped. */
+rgnn_status_t rgnn_clip_workspace_bytes(int64_t count, const int64_t* sizes, size_t* workspace);
+rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* grads, void* const* clipped, const int64_t* sizes,
+                                  const int32_t* dtypes, float max_norm, float* norm, void* workspace, void* stream);
 
 /*
  * Per-kernel timing for benchmarks (not part of the layer definition).  Between

@@ -18,7 +18,7 @@ RGNN_OK = 0
 RGNN_F32, RGNN_BF16 = 0, 1
 RGNN_LAYER_RGCN, RGNN_LAYER_RGAT, RGNN_LAYER_HGT = 0, 1, 2
 RGNN_NORM_NONE, RGNN_NORM_IN_DEGREE_PER_REL = 0, 1
-RGNN_ACT_NONE, RGNN_ACT_RELU = 0, 1
+RGNN_ACT_NONE, RGNN_ACT_RELU, RGNN_ACT_SILU = 0, 1, 2
 RGNN_FLAG_EDGE_PARALLEL_AGGREGATION = 1
 RGNN_FLAG_NO_BATCHED_WALKS = 2
 RGNN_FLAG_NO_ROW_SELECT = 4
@@ -36,7 +36,9 @@ INDEX_NAMES = ["in_ptr", "in_src", "in_rel", "in_eid", "in_pair", "in_run", "in_
 
 EXPORTS = ["rgnn_last_error", "rgnn_graph_create", "rgnn_graph_destroy", "rgnn_graph_info", "rgnn_graph_export",
            "rgnn_workspace_bytes", "rgnn_rgcn_fwd", "rgnn_rgcn_bwd", "rgnn_rgat_fwd", "rgnn_rgat_bwd",
-           "rgnn_hgt_fwd", "rgnn_hgt_bwd", "rgnn_profile_start", "rgnn_profile_stop", "rgnn_profile_select", "rgnn_rgat_fwd_static", "rgnn_schedule"]
+           "rgnn_hgt_fwd", "rgnn_hgt_bwd", "rgnn_profile_start", "rgnn_profile_stop", "rgnn_profile_select", "rgnn_rgat_fwd_static", "rgnn_schedule",
+           "rgnn_norm_workspace_bytes", "rgnn_norm_fwd", "rgnn_norm_bwd", "rgnn_ffn_workspace_bytes", "rgnn_ffn_fwd", "rgnn_ffn_bwd",
+           "rgnn_clip_workspace_bytes", "rgnn_clip_grad_norm"]
 
 
 class RgnnError(RuntimeError):
@@ -55,6 +57,16 @@ class GraphInfo(C.Structure):
 class LayerDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("d_in", C.c_int32), ("d_out", C.c_int32), ("heads", C.c_int32),
                 ("slope", C.c_float), ("norm", C.c_int32), ("activation", C.c_int32), ("flags", C.c_uint32)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("x_dtype", C.c_int32), ("sum_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("eps", C.c_float), ("flags", C.c_uint32)]
+
+
+class FfnDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("dtype", C.c_int32), ("width", C.c_int32), ("hidden", C.c_int32), ("activation", C.c_int32),
+                ("flags", C.c_uint32)]
 
 
 class Schedule(C.Structure):
@@ -179,6 +191,60 @@ def rgnn_hgt_bwd(g, desc, X, Wk, Wq, Wv, Wo, Watt, Wmsg, mu, out, saved, dOut, d
                               _ptr(Wmsg), _ptr(mu), _ptr(out), _ptr(saved), _ptr(dOut), _ptr(dX), _ptr(dWk),
                               _ptr(dWq), _ptr(dWv), _ptr(dWo), _ptr(dWatt), _ptr(dWmsg), _ptr(dmu),
                               _ptr(workspace), _ptr(stream)))
+
+
+def make_norm_desc(rows, width, x_dtype=RGNN_F32, sum_dtype=RGNN_F32, out_dtype=RGNN_F32, eps=1e-6, flags=0):
+    return NormDesc(rows, width, x_dtype, sum_dtype, out_dtype, eps, flags)
+
+
+def rgnn_norm_workspace_bytes(desc):
+    b = C.c_size_t()
+    _check(lib().rgnn_norm_workspace_bytes(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def rgnn_norm_fwd(desc, x, residual, weight, sum, out, stream=None):
+    _check(lib().rgnn_norm_fwd(C.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum), _ptr(out), _ptr(stream)))
+
+
+def rgnn_norm_bwd(desc, sum, weight, dOut, dSum, dX, dResidual, dWeight, workspace, stream=None):
+    _check(lib().rgnn_norm_bwd(C.byref(desc), _ptr(sum), _ptr(weight), _ptr(dOut), _ptr(dSum), _ptr(dX), _ptr(dResidual),
+                               _ptr(dWeight), _ptr(workspace), _ptr(stream)))
+
+
+def make_ffn_desc(rows, width, hidden, dtype=RGNN_F32, activation=RGNN_ACT_SILU, flags=0):
+    return FfnDesc(rows, dtype, width, hidden, activation, flags)
+
+
+def rgnn_ffn_workspace_bytes(desc):
+    """-> (forward, backward) workspace bytes."""
+    f, b = C.c_size_t(), C.c_size_t()
+    _check(lib().rgnn_ffn_workspace_bytes(C.byref(desc), C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
+def rgnn_ffn_fwd(desc, X, Wg, Wu, Wd, out, workspace, stream=None):
+    _check(lib().rgnn_ffn_fwd(C.byref(desc), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(out), _ptr(workspace), _ptr(stream)))
+
+
+def rgnn_ffn_bwd(desc, X, Wg, Wu, Wd, dOut, dX, dWg, dWu, dWd, workspace, stream=None):
+    _check(lib().rgnn_ffn_bwd(C.byref(desc), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(dOut), _ptr(dX), _ptr(dWg), _ptr(dWu),
+                              _ptr(dWd), _ptr(workspace), _ptr(stream)))
+
+
+def rgnn_clip_workspace_bytes(sizes):
+    b = C.c_size_t()
+    n = len(sizes)
+    _check(lib().rgnn_clip_workspace_bytes(C.c_int64(n), (C.c_int64 * n)(*sizes), C.byref(b)))
+    return b.value
+
+
+def rgnn_clip_grad_norm(grads, clipped, sizes, dtypes, max_norm, norm, workspace, stream=None):
+    """grads, clipped: lists of torch tensors or raw pointers; clipped may be None (the norm alone)."""
+    n = len(grads)
+    addr = lambda ts: (C.c_void_p * n)(*[t if isinstance(t, int) or t is None else t.data_ptr() for t in ts])
+    _check(lib().rgnn_clip_grad_norm(C.c_int64(n), addr(grads), None if clipped is None else addr(clipped), (C.c_int64 * n)(*sizes),
+                                     (C.c_int32 * n)(*dtypes), C.c_float(max_norm), _ptr(norm), _ptr(workspace), _ptr(stream)))
 
 
 def rgnn_profile_select(name=None):

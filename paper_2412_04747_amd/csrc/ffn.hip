@@ -1,0 +1,367 @@
+// Gated feed-forward block: entry points, the forward, and the gradient of the rows (ffn.h has the formulas).
+//
+// A wavefront keeps 32 rows of X (and of dOut) in registers as the second operand of every product, so that results come out with the
+// rows along the lanes: chunk by chunk of 32 hidden values it forms g^T = Wg^T X^T and u^T (dh^T = Wd dOut^T), applies the activation
+// where they lie, and adds Wd^T h^T to its result (Wg dg^T + Wu du^T).  The weights, first laid out by a small launch in the
+// order in which the instructions read them (as planes, padded with zeros to whole chunks), come through the LDS for the four
+// wavefronts of a workgroup in two halves that take turns: while one is multiplied the other is on its way.
+// Nothing of the hidden width is written.  Matrix instructions bound it: 6 (10) N d f operations, sixfold for fp32.
+// With few rows the chunks are divided among workgroups too, and a last launch adds their shares in order.
+#include <math.h>
+
+#include "rgnn_internal.h"
+#include "device_utils.h"
+#include "ffn.h"
+
+namespace rgnn {
+
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kFrag = 1024;              // bytes of an operand of a wavefront's instruction
+
+// Sections of a chunk, each D / 16 operands of PL planes.  Forward: gate, up, down.  Backward: gate, up, out, gate back, up back.
+enum { kGate, kUp, kDown, kOut, kGateBack, kUpBack };
+
+// One lane's eight values of an operand.
+struct PackArgs { int hidden, chunks, backward; const void* Wg; const void* Wu; const void* Wd; unsigned char* to; };
+template <int D, int PL>
+__global__ __launch_bounds__(256) void ffn_pack_kernel(PackArgs a) {
+    constexpr int S = D / 16;
+    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
+    const int sections = a.backward ? 5 : 3;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int lane = (int)(id & 63), s = (int)((id >> 6) % S);
+    const int64_t q = (id >> 6) / S;
+    const int sec = (int)(q % sections);
+    const int64_t chunk = q / sections;
+    if (chunk >= a.chunks) return;
+    const int what = a.backward ? (sec == 2 ? kOut : sec == 3 ? kGateBack : sec == 4 ? kUpBack : sec) : sec;
+    const int m = lane & 31, kh = lane >> 5, F = a.hidden;
+    const T* W = static_cast<const T*>(what == kGate || what == kGateBack ? a.Wg : what == kUp || what == kUpBack ? a.Wu : a.Wd);
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        int h, c;                        // hidden value, column of the row
+        if (what == kGate || what == kUp || what == kOut) {
+            h = (int)chunk * kHid + m;
+            c = 16 * s + 8 * kh + j;
+        } else {                         // operand s: columns 32 (s / 2) + m, the (s % 2)-th 16 hidden values in the order of an accumulator
+            h = (int)chunk * kHid + 16 * (s & 1) + 8 * (j >> 2) + 4 * kh + (j & 3);
+            c = 32 * (s >> 1) + m;
+        }
+        const bool down = what == kDown || what == kOut;
+        v[j] = h < F ? widen(W[down ? (size_t)h * D + c : (size_t)c * F + h]) : 0.f;
+    }
+    bf16x8 p[PL];
+    planes8<PL>(v, p);
+    unsigned char* const to = a.to + (((chunk * sections + sec) * S + s) * PL) * kFrag + lane * 16;
+#pragma unroll
+    for (int k = 0; k < PL; ++k) *reinterpret_cast<bf16x8*>(to + k * kFrag) = p[k];
+}
+
+// n operands from memory into the LDS, by all wavefronts of the workgroup
+__device__ __forceinline__ void fetch(const unsigned char* from, unsigned char* lds, int n) {
+    const int lane = threadIdx.x & 63;
+    for (int k = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); k < n; k += kWaves)
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (size_t)k * kFrag + lane * 16),
+                                         (__attribute__((address_space(3))) void*)(lds + k * kFrag), 16, 0, 0);
+}
+// what this wavefront has under way has arrived, then all have
+__device__ __forceinline__ void arrived() {
+    __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
+    __syncthreads();
+}
+
+template <int PL>
+__device__ __forceinline__ void operand(const unsigned char* at, bf16x8 (&f)[PL]) {
+#pragma unroll
+    for (int k = 0; k < PL; ++k) f[k] = *reinterpret_cast<const bf16x8*>(at + k * kFrag + (threadIdx.x & 63) * 16);
+}
+
+struct RowsArgs {
+    FfnArgs a;
+    const unsigned char* packed;
+    void* out;               // rows of the result
+    float* part;             // with several splits: [splits][rows][D]
+    int splits, accumulate;
+};
+
+// The lane's row of the result: tile t holds columns 32 t + 8 q + 4 kh + (0..3) in values 4 q .. 4 q + 3.
+template <int D, int PL>
+__device__ __forceinline__ void store_result(const RowsArgs& r, int64_t row, int kh, const v16f (&y)[D / 32]) {
+    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
+    if (row >= r.a.rows) return;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[4] = {y[t][4 * q], y[t][4 * q + 1], y[t][4 * q + 2], y[t][4 * q + 3]};
+            const int64_t at = row * D + 32 * t + 8 * q + 4 * kh;
+            if (r.splits > 1) {
+                store_cols<4>(r.part + (int64_t)blockIdx.y * r.a.rows * D + at, v);
+            } else {
+                T* const p = static_cast<T*>(r.out) + at;
+                if (r.accumulate) {
+                    float o[4];
+                    load_cols<4>(p, o);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += o[e];
+                }
+                store_cols<4>(p, v);
+            }
+        }
+}
+
+template <int D, int PL, int ACT, int RT, bool BWD>
+__global__ __launch_bounds__(64 * kWaves, 1) void ffn_rows_kernel(RowsArgs r) {
+    constexpr int S = D / 16, TILES = D / 32, OPS = S * PL, FIRST = (BWD ? 3 : 2) * OPS, SECOND = (BWD ? 2 : 1) * OPS;
+    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
+    extern __shared__ unsigned char lds[];
+    unsigned char* const first = lds;
+    unsigned char* const second = lds + FIRST * kFrag;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
+    const int64_t row0 = ((int64_t)blockIdx.x * kWaves + wave) * (32 * RT) + m;
+    const int c0 = (int)((int64_t)r.a.chunks * blockIdx.y / r.splits), c1 = (int)((int64_t)r.a.chunks * (blockIdx.y + 1) / r.splits);
+    const unsigned char* from = r.packed + (size_t)c0 * (FIRST + SECOND) * kFrag;
+    fetch(from, first, FIRST);
+
+    bf16x8 x[RT][S][PL], dy[BWD ? RT : 1][BWD ? S : 1][PL];
+    v16f y[RT][TILES];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int64_t row = row0 + 32 * i;
+        const bool ok = row < r.a.rows;
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            load_planes8<PL>(static_cast<const T*>(r.a.X) + row * D + 16 * s + 8 * kh, ok, x[i][s]);
+            if constexpr (BWD) load_planes8<PL>(static_cast<const T*>(r.a.dOut) + row * D + 16 * s + 8 * kh, ok, dy[i][s]);
+        }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) clear(y[i][t]);
+    }
+    for (int c = c0; c < c1; ++c, from += (size_t)(FIRST + SECOND) * kFrag) {
+        arrived();
+        fetch(from + (size_t)FIRST * kFrag, second, SECOND);
+        v16f g[RT], u[RT], dh[BWD ? RT : 1];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            clear(g[i]);
+            clear(u[i]);
+            if constexpr (BWD) clear(dh[i]);
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            bf16x8 wg[PL], wu[PL];
+            operand(first + s * PL * kFrag, wg);
+            operand(first + (S + s) * PL * kFrag, wu);
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                mul_add<PL>(wg, x[i][s], g[i]);
+                mul_add<PL>(wu, x[i][s], u[i]);
+            }
+            if constexpr (BWD) {
+                bf16x8 wd[PL];
+                operand(first + (2 * S + s) * PL * kFrag, wd);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) mul_add<PL>(wd, dy[i][s], dh[i]);
+            }
+        }
+        arrived();
+        if (c + 1 < c1) fetch(from + (size_t)(FIRST + SECOND) * kFrag, first, FIRST);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 p[RT][PL], p2[BWD ? RT : 1][PL];
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                float v[8], v2[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float gv = g[i][8 * s + j], uv = u[i][8 * s + j];
+                    if constexpr (BWD) {
+                        float av, slope;
+                        act_slope<ACT>(gv, av, slope);
+                        v[j] = dh[i][8 * s + j] * uv * slope;
+                        v2[j] = dh[i][8 * s + j] * av;
+                    } else {
+                        v[j] = act<ACT>(gv) * uv;
+                    }
+                }
+                planes8<PL>(v, p[i]);
+                if constexpr (BWD) planes8<PL>(v2, p2[i]);
+            }
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                bf16x8 w[PL];
+                operand(second + (2 * t + s) * PL * kFrag, w);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) mul_add<PL>(w, p[i], y[i][t]);
+                if constexpr (BWD) {
+                    operand(second + (S + 2 * t + s) * PL * kFrag, w);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) mul_add<PL>(w, p2[i], y[i][t]);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) store_result<D, PL>(r, row0 + 32 * i, kh, y[i]);
+}
+
+// The splits' shares, added in order.  Four columns per thread.
+template <typename T>
+__global__ __launch_bounds__(256) void ffn_combine_kernel(const float* part, int splits, int64_t n, T* out, int accumulate) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    float s[4];
+    zero_cols<4>(s);
+    if (accumulate) load_cols<4>(out + i, s);
+    float sum[4];
+    zero_cols<4>(sum);
+    for (int k = 0; k < splits; ++k) {
+        float v[4];
+        load_cols<4>(part + k * n + i, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += sum[e];
+    store_cols<4>(out + i, s);
+}
+
+int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
+// Wavefronts take 32 rows, or 64 where the operands of 64 fit their registers: the weights then cross the LDS half as often.
+int row_tiles(const rgnn_ffn_desc_t* d, bool) { return d->dtype == RGNN_BF16 && d->rows >= 65536 ? 2 : 1; }
+// One workgroup per compute unit at least, as far as the chunks go.
+int splits_of(const rgnn_ffn_desc_t* d, bool backward) {
+    const int64_t blocks = (d->rows + 32 * kWaves * row_tiles(d, backward) - 1) / (32 * kWaves * row_tiles(d, backward));
+    return blocks >= 256 || blocks == 0 ? 1 : (int)std::min<int64_t>(chunks_of(d), (256 + blocks - 1) / blocks);
+}
+size_t packed_bytes(const rgnn_ffn_desc_t* d, bool backward) {
+    return align_up((size_t)chunks_of(d) * (backward ? 5 : 3) * (d->width / 16) * (d->dtype == RGNN_BF16 ? 1 : 3) * kFrag);
+}
+size_t share_bytes(const rgnn_ffn_desc_t* d, bool backward) {
+    const int s = splits_of(d, backward);
+    return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
+}
+size_t grad_bytes(const rgnn_ffn_desc_t* d) {
+    return align_up(sizeof(float) * (size_t)ffn_grad_splits(d) * 3 * d->width * chunks_of(d) * kHid);
+}
+
+template <int D, int PL, int ACT, int RT, bool BWD>
+rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
+    constexpr size_t lds = (size_t)(BWD ? 5 : 3) * (D / 16) * PL * kFrag;
+    auto* const kernel = ffn_rows_kernel<D, PL, ACT, RT, BWD>;
+    RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
+    const int64_t per = 32 * kWaves * RT;
+    KernelTimer timer(st, BWD ? "ffn_bwd_rows" : "ffn_fwd");
+    kernel<<<dim3((unsigned)((r.a.rows + per - 1) / per), r.splits), 64 * kWaves, lds, st>>>(r);
+    RGNN_CHECK_LAUNCH();
+    return RGNN_OK;
+}
+
+template <bool BWD>
+rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, int accumulate, void* workspace, hipStream_t st) {
+    unsigned char* const packed = static_cast<unsigned char*>(workspace);
+    const RowsArgs r{a, packed, out, reinterpret_cast<float*>(packed + packed_bytes(d, BWD)), splits_of(d, BWD), accumulate};
+    auto run = [&]() -> rgnn_status_t {
+        RGNN_DISPATCH_FFN(d, {
+            {
+                const PackArgs p{a.hidden, a.chunks, BWD, a.Wg, a.Wu, a.Wd, packed};
+                const int64_t threads = (int64_t)a.chunks * (BWD ? 5 : 3) * (D / 16) * 64;
+                KernelTimer timer(st, "ffn_pack");
+                ffn_pack_kernel<D, PL><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(p);
+                RGNN_CHECK_LAUNCH();
+            }
+            if constexpr (PL == 1) {
+                if (row_tiles(d, BWD) == 2) return launch_rows<D, PL, ACT, 2, BWD>(r, st);
+            }
+            return launch_rows<D, PL, ACT, 1, BWD>(r, st);
+        });
+    };
+    RGNN_TRY(run());
+    if (r.splits > 1) {
+        const int64_t n = a.rows * d->width;
+        KernelTimer timer(st, "ffn_combine");
+        const unsigned blocks = (unsigned)((n / 4 + 255) / 256);
+        if (d->dtype == RGNN_BF16) ffn_combine_kernel<<<blocks, 256, 0, st>>>(r.part, r.splits, n, static_cast<bf16_t*>(out), accumulate);
+        else ffn_combine_kernel<<<blocks, 256, 0, st>>>(r.part, r.splits, n, static_cast<float*>(out), accumulate);
+        RGNN_CHECK_LAUNCH();
+    }
+    return RGNN_OK;
+}
+
+rgnn_status_t check_desc(const rgnn_ffn_desc_t* d) {
+    if (!d) RGNN_FAIL(RGNN_EINVAL, "desc is NULL");
+    RGNN_TRY(check_rows(d->rows));
+    RGNN_TRY(check_dtype(d->dtype));
+    
+    if (d->width != 32 && d->width != 64 && d->width != 128) RGNN_FAIL(RGNN_EUNSUPPORTED, "width %d not supported (32/64/128)", d->width);
+    if (d->hidden < 1) RGNN_FAIL(RGNN_EINVAL, "hidden %d is not positive", d->hidden);
+    if (d->hidden > 16384) RGNN_FAIL(RGNN_EUNSUPPORTED, "hidden %d not supported (up to 16384)", d->hidden);
+    if (d->activation != RGNN_ACT_RELU && d->activation != RGNN_ACT_SILU) RGNN_FAIL(RGNN_EINVAL, "unknown activation %d", d->activation);
+    if (d->flags & ~RGNN_FLAG_ACCUMULATE) RGNN_FAIL(RGNN_EINVAL, "flags: only RGNN_FLAG_ACCUMULATE applies");
+    return RGNN_OK;
+}
+
+// No written tensor shares memory with another one; all are aligned.
+rgnn_status_t check_tensors(std::initializer_list<Span> read, std::initializer_list<Span> written) {
+    for (const Span& s : read) RGNN_TRY(check_aligned(s));
+    for (const Span* w = written.begin(); w != written.end(); ++w) {
+        RGNN_TRY(check_aligned(*w));
+        for (const Span& s : read)
+            if (w->overlaps(s)) RGNN_FAIL(RGNN_EINVAL, "an output or the workspace overlaps an input");
+        for (const Span* v = written.begin(); v != w; ++v)
+            if (w->overlaps(*v)) RGNN_FAIL(RGNN_EINVAL, "two outputs, or one and the workspace, overlap");
+    }
+    return RGNN_OK;
+}
+
+}  // namespace
+
+}  // namespace rgnn
+
+using namespace rgnn;
+
+extern "C" rgnn_status_t rgnn_ffn_workspace_bytes(const rgnn_ffn_desc_t* desc, size_t* fwd_workspace, size_t* bwd_workspace) {
+    RGNN_TRY(check_desc(desc));
+    if (fwd_workspace) *fwd_workspace = packed_bytes(desc, false) + share_bytes(desc, false);
+    if (bwd_workspace) *bwd_workspace = std::max(packed_bytes(desc, true) + share_bytes(desc, true), grad_bytes(desc));
+    return RGNN_OK;
+}
+
+extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, void* out,
+                                      void* workspace, void* stream) {
+    RGNN_TRY(check_desc(desc));
+    if (desc->rows == 0) return RGNN_OK;
+    if (!X || !Wg || !Wu || !Wd || !out) RGNN_FAIL(RGNN_EINVAL, "X, a weight or out is NULL");
+    if (!workspace) RGNN_FAIL(RGNN_EWORKSPACE, "workspace is NULL");
+    const size_t n = (size_t)desc->rows * desc->width, w = (size_t)desc->hidden * desc->width;
+    const int32_t t = desc->dtype;
+    RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t)},
+                           {span(out, n, t), Span{static_cast<char*>(workspace), packed_bytes(desc, false) + share_bytes(desc, false)}}));
+    const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, nullptr};
+    return rows_pass<false>(desc, a, out, 0, workspace, static_cast<hipStream_t>(stream));
+}
+
+extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
+                                      void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream) {
+    RGNN_TRY(check_desc(desc));
+    const bool grads = dWg || dWu || dWd;
+    if (grads && !(dWg && dWu && dWd)) RGNN_FAIL(RGNN_EINVAL, "dWg, dWu and dWd are given together or not at all");
+    if (!Wg || !Wu || !Wd) RGNN_FAIL(RGNN_EINVAL, "a weight is NULL");
+    if (desc->rows > 0 && (!X || !dOut)) RGNN_FAIL(RGNN_EINVAL, "X or dOut is NULL");
+    if (!workspace) RGNN_FAIL(RGNN_EWORKSPACE, "workspace is NULL");
+    const size_t n = (size_t)desc->rows * desc->width, w = (size_t)desc->hidden * desc->width;
+    const int32_t t = desc->dtype;
+    size_t bytes = 0;
+    RGNN_TRY(rgnn_ffn_workspace_bytes(desc, nullptr, &bytes));
+    RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t), span(dOut, n, t)},
+                           {span(dX, n, t), span(dWg, w, t), span(dWu, w, t), span(dWd, w, t), Span{static_cast<char*>(workspace), bytes}}));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, dOut};
+    const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
+    if (dX && desc->rows > 0) RGNN_TRY(rows_pass<true>(desc, a, dX, accumulate, workspace, st));
+    if (grads && (desc->rows > 0 || !accumulate)) RGNN_TRY(ffn_grad(desc, a, static_cast<float*>(workspace), dWg, dWu, dWd, st));
+    return RGNN_OK;
+}

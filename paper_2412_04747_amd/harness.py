@@ -180,3 +180,61 @@ class HgtLayer:
         if self.dmu is not None:
             g["dmu"] = self.dmu
         return g
+
+
+class NormLayer:
+    """Device buffers for one residual norm call pair on `rows` rows.  `x`, `residual`, `weight` (and `dOut`, `dSum`) are set by the
+    caller; types "f32" or "bf16".  Without a residual, `total` is `x`'s type and the backward's `sum` is x."""
+
+    def __init__(self, rows, width, x="f32", total="f32", out="f32", eps=1e-6, residual=True, flags=0):
+        (cx, tx), (cs, ts), (co, to) = _tdtype(x), _tdtype(total), _tdtype(out)
+        self.desc = B.make_norm_desc(rows, width, cx, cs, co, eps, flags)
+        self.ws = _buf(B.rgnn_norm_workspace_bytes(self.desc))
+        e = lambda t: torch.empty(rows, width, device="cuda", dtype=t)
+        self.residual = self.dSum = None
+        self.out, self.sum = e(to), e(ts) if residual else None
+        # one buffer where the gradients of x and of the residual are of one type
+        self.dResidual = e(ts) if residual else None
+        self.dX = e(tx) if not residual or tx != ts else None
+        self.dWeight = torch.empty(width, device="cuda")
+
+    def fwd(self):
+        B.rgnn_norm_fwd(self.desc, self.x, self.residual, self.weight, self.sum, self.out, _stream())
+
+    def bwd(self):
+        B.rgnn_norm_bwd(self.desc, self.sum, self.weight, self.dOut, self.dSum, self.dX, self.dResidual, self.dWeight, self.ws, _stream())
+
+
+class FfnLayer:
+    """Device buffers for one feed-forward block call pair on `rows` rows.  `X`, `Wg`, `Wu`, `Wd` (and `dOut`) are set by the caller."""
+
+    def __init__(self, rows, width, hidden, dtype="f32", act="silu", flags=0):
+        code, t = _tdtype(dtype)
+        self.desc = B.make_ffn_desc(rows, width, hidden, code, B.RGNN_ACT_RELU if act == "relu" else B.RGNN_ACT_SILU, flags)
+        self.ws = _buf(max(B.rgnn_ffn_workspace_bytes(self.desc)))
+        e = lambda *shape: torch.empty(*shape, device="cuda", dtype=t)
+        self.out, self.dX = e(rows, width), e(rows, width)
+        self.dWg, self.dWu, self.dWd = e(width, hidden), e(width, hidden), e(hidden, width)
+
+    def fwd(self):
+        B.rgnn_ffn_fwd(self.desc, self.X, self.Wg, self.Wu, self.Wd, self.out, self.ws, _stream())
+
+    def bwd(self):
+        B.rgnn_ffn_bwd(self.desc, self.X, self.Wg, self.Wu, self.Wd, self.dOut, self.dX, self.dWg, self.dWu, self.dWd, self.ws, _stream())
+
+    def grads(self):
+        return dict(dX=self.dX, dWg=self.dWg, dWu=self.dWu, dWd=self.dWd)
+
+
+class GradClip:
+    """The workspace and result buffers for clipping tensors of the sizes and types of `like`, in place or into `clipped`."""
+
+    def __init__(self, like, in_place=True):
+        self.sizes = [t.numel() for t in like]
+        self.dtypes = [B.RGNN_BF16 if t.dtype == torch.bfloat16 else B.RGNN_F32 for t in like]
+        self.ws = _buf(B.rgnn_clip_workspace_bytes(self.sizes))
+        self.norm = torch.empty((), device="cuda")
+        self.clipped = None if in_place else [torch.empty_like(t) for t in like]
+
+    def clip(self, grads, max_norm):
+        B.rgnn_clip_grad_norm(grads, self.clipped or grads, self.sizes, self.dtypes, max_norm, self.norm, self.ws, _stream())

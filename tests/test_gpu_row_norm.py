@@ -1,0 +1,212 @@
+"""Residual addition with root-mean-square norm against its definition in 64 bits.
+
+Tolerances, per element: a stored value is off by half a step of its type, eps / 2 of its magnitude.  In fp32 the sum x + r rounds once, the
+mean of squares (all terms positive) at most once per term of a lane (16), per step of the lanes' tree (6) and per wavefront (8), the
+reciprocal root takes half of that, and the products three roundings: 32 units of 2^-24 in all, of |out|.  The backward has differences:
+the same units apply to the sum of its terms' magnitudes, and the mean of g s to that of |g s|.  dw adds one rounding per row that a group of
+lanes walks, then a tree."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-6
+U = 2.0 ** -24
+
+
+def _t(name):
+    import torch
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _half(name):
+    return 2.0 ** -8 if name == "bf16" else U
+
+
+def _inputs(rows, width, x, total, out, residual, seed):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    n = lambda scale, t: (torch.randn(rows, width, generator=g) * scale).to(_t(t))
+    d = dict(x=n(1.0, x), w=1.0 + 0.2 * torch.randn(width, generator=g), r=n(2.0, total) if residual else None, dy=n(0.1, out),
+             ds=n(0.1, total) if residual else None)
+    if rows > 2:
+        d["x"][1] = 0                                    # a row of zeros, as a layer gives for a node without edges
+        if residual:
+            d["r"][1] = 0
+    return d
+
+
+def _layer(d, rows, width, x, total, out, residual, flags=0):
+    from paper_2412_04747_amd.harness import NormLayer
+    L = NormLayer(rows, width, x, total, out, EPS, residual=residual, flags=flags)
+    c = lambda t: None if t is None else t.cuda()
+    L.x, L.residual, L.weight, L.dOut, L.dSum = c(d["x"]), c(d["r"]), c(d["w"]), c(d["dy"]), c(d["ds"])
+    return L
+
+
+def _within(got, want, tol, what):
+    got = got.detach().cpu().double().numpy()
+    off = np.abs(got - want)
+    bad = ~(off <= tol)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size}, first at {np.argwhere(bad)[0]}: off {off[bad][0]:.3e}, allowed {np.broadcast_to(tol, off.shape)[bad][0]:.3e}"
+
+
+CASES = [(1, 1), (1, 64), (3, 2), (17, 3), (5, 31), (33, 32), (1000, 64), (129, 100), (64, 128), (41, 255), (30, 349), (77, 512), (9, 1000),
+         (6, 1021), (12, 2048), (5, 2052), (3, 4099), (4, 8192), (2, 8191), (20011, 64)]
+TYPES = [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "f32", "bf16"), ("bf16", "f32", "f32"), ("f32", "bf16", "bf16"),
+         ("bf16", "f32", "bf16"), ("bf16", "bf16", "f32"), ("f32", "bf16", "f32")]
+
+
+@pytest.mark.parametrize("i,rows,width", [(i, *c) for i, c in enumerate(CASES)])
+@pytest.mark.parametrize("residual", [True, False])
+def test_against_the_definition(i, rows, width, residual):
+    import torch
+    for x, total, out in [TYPES[i % 8], TYPES[(i + 3) % 8]] if rows * width < 100000 else [TYPES[0], TYPES[1]]:
+        if not residual:
+            total = x
+        print(f"norm case rows={rows} width={width} types {x} {total} {out} residual={residual}", flush=True)
+        d = _inputs(rows, width, x, total, out, residual, 7 * rows + width)
+        L = _layer(d, rows, width, x, total, out, residual)
+        L.fwd()
+        torch.cuda.synchronize()
+        f = lambda t: t.double().numpy()
+        s = f(d["x"]) + (f(d["r"]) if residual else 0.0)
+        q = 1.0 / np.sqrt((s * s).mean(1, keepdims=True) + EPS)
+        want = s * q * f(d["w"])
+        _within(L.out, want, np.abs(want) * (_half(out) + 32 * U) + 1e-30, "out")
+        if residual:
+            _within(L.sum, s, np.abs(s) * (_half(total) + U), "sum")
+        kept = L.sum if residual else L.x
+        L.sum = kept
+        L.bwd()
+        torch.cuda.synchronize()
+        s, dy, w = kept.cpu().double().numpy(), f(d["dy"]), f(d["w"])
+        ds = f(d["ds"]) if residual else np.zeros_like(s)
+        q = 1.0 / np.sqrt((s * s).mean(1, keepdims=True) + EPS)
+        g = dy * w
+        dx = ds + q * (g - s * q * q * (g * s).mean(1, keepdims=True))
+        size = np.abs(ds) + q * (np.abs(g) + np.abs(s) * q * q * np.abs(g * s).mean(1, keepdims=True))
+        for t, what, kind in ((L.dX, "dX", x), (L.dResidual, "dResidual", total)):
+            if t is not None:
+                _within(t, dx, np.abs(dx) * _half(kind) + size * 48 * U + 1e-30, what)
+        _within(L.dWeight, (dy * s * q).sum(0), np.abs(dy * s * q).sum(0) * (64 + rows / 512) * U + 1e-30, "dWeight")
+
+
+def test_gradient_against_differences():
+    """The backward's formula against central differences of the forward's, both in 64 bits, and the kernel against either: 20 rows."""
+    import torch
+    rows, width = 20, 33
+    d = _inputs(rows, width, "f32", "f32", "f32", True, 5)
+    L = _layer(d, rows, width, "f32", "f32", "f32", True)
+    L.fwd(); L.bwd()
+    torch.cuda.synchronize()
+    s, w, dy, ds = L.sum.cpu().double(), d["w"].double(), d["dy"].double(), d["ds"].double()
+
+    def loss(s, w):
+        return float((s / torch.sqrt((s * s).mean(1, keepdim=True) + EPS) * w * dy).sum() + (s * ds).sum())
+
+    h = 1e-6
+    for i, j in [(0, 0), (3, 7), (19, 32), (10, 1), (2, 30)]:
+        a, b = s.clone(), s.clone()
+        a[i, j] += h
+        b[i, j] -= h
+        # differences of step h in 64 bits: 1e-9 or so off
+        assert abs((loss(a, w) - loss(b, w)) / (2 * h) - float(L.dResidual[i, j])) < 1e-6
+    for j in (0, 15, 32):
+        a, b = w.clone(), w.clone()
+        a[j] += h
+        b[j] -= h
+        assert abs((loss(s, a) - loss(s, b)) / (2 * h) - float(L.dWeight[j])) < 1e-5
+
+
+def test_in_place_and_repeatable():
+    import torch
+    rows, width = 1003, 64
+    d = _inputs(rows, width, "f32", "f32", "f32", True, 9)
+    L = _layer(d, rows, width, "f32", "f32", "f32", True)
+    L.fwd(); L.bwd()
+    want = [t.clone() for t in (L.sum, L.out, L.dResidual, L.dWeight)]
+    M = _layer(d, rows, width, "f32", "f32", "f32", True)
+    M.sum, M.out = M.residual, M.x                       # the stream and the addend are written over
+    M.fwd()
+    M.dResidual = M.dSum
+    M.bwd()
+    for a, b in zip((M.sum, M.out, M.dResidual, M.dWeight), want):
+        assert torch.equal(a, b)
+
+
+def test_accumulate_and_optional_results():
+    import torch
+    from paper_2412_04747_amd import binding as B
+    rows, width = 515, 96
+    for x, total in (("f32", "f32"), ("bf16", "f32")):
+        d = _inputs(rows, width, x, total, "bf16", True, 11)
+        L = _layer(d, rows, width, x, total, "bf16", True)
+        L.fwd(); L.bwd()
+        M = _layer(d, rows, width, x, total, "bf16", True, flags=B.RGNN_FLAG_ACCUMULATE)
+        M.sum = L.sum
+        for t in (M.dX, M.dResidual, M.dWeight):
+            if t is not None:
+                t.fill_(1.0)
+        M.bwd()
+        assert torch.equal(M.dWeight, L.dWeight + 1.0)
+        for a, b in ((M.dX, L.dX), (M.dResidual, L.dResidual)):
+            # a = round(v + 1), b = round(v): half a step of either, of magnitudes up to 1 + |v| (300 in the row of zeros, where
+            # the norm multiplies by 1 / sqrt(eps)); |v| <= 1.01 |b| + 1e-30
+            if a is not None:
+                step = U if a.dtype == torch.float32 else 2.0 ** -8
+                assert ((a.double() - (b.double() + 1.0)).abs() <= 2.1 * step * (1.0 + b.double().abs())).all()
+        # any of the results may be left out
+        L.dX = L.dResidual = None
+        keep = L.dWeight.clone()
+        L.bwd()
+        assert torch.equal(L.dWeight, keep)
+    # no rows: the weight's gradient is zeros, or stays
+    N = _layer(_inputs(0, 96, "f32", "f32", "f32", True, 1), 0, 96, "f32", "f32", "f32", True)
+    N.dWeight.fill_(3.0)
+    N.fwd(); N.bwd()
+    assert (N.dWeight == 0).all()
+    N.desc.flags = B.RGNN_FLAG_ACCUMULATE
+    N.dWeight.fill_(3.0)
+    N.bwd()
+    assert (N.dWeight == 3.0).all()
+
+
+@pytest.mark.parametrize("width", [64, 349, 4096])
+def test_bad_rows_stay_alone(width):
+    """A row with an infinity or NaN does not touch the others, and nothing is written behind the last row."""
+    import torch
+    rows = 70
+    d = _inputs(rows, width, "f32", "f32", "f32", True, 13)
+    L = _layer(d, rows, width, "f32", "f32", "f32", True)
+    L.fwd(); L.bwd()
+    out, dr = L.out.clone(), L.dResidual.clone()
+    M = _layer(d, rows, width, "f32", "f32", "f32", True)
+    M.x[5, width - 1], M.x[40, 0] = float("nan"), float("inf")
+    big = [torch.full((rows + 8, width), 7.0, device="cuda") for _ in range(2)]
+    M.sum, M.out = big[0][:rows], big[1][:rows]
+    M.fwd(); M.bwd()
+    good = [i for i in range(rows) if i not in (5, 40)]
+    assert torch.equal(M.out[good], out[good]) and torch.equal(M.dResidual[good], dr[good])
+    assert M.out[5].isnan().all() and M.out[40, 0].isnan()
+    assert all((b[rows:] == 7.0).all() for b in big)
+
+
+def test_more_than_32_bits_of_elements():
+    """Rows past 2^31 elements: the same as those rows alone."""
+    import torch
+    rows, width = (1 << 24) + 5, 128
+    from paper_2412_04747_amd.harness import NormLayer
+    print(f"norm case rows={rows} width={width}", flush=True)
+    L = NormLayer(rows, width, "bf16", "bf16", "bf16", EPS, residual=False)
+    L.x = torch.empty(rows, width, device="cuda", dtype=torch.bfloat16)
+    L.x.normal_()
+    L.weight = torch.linspace(0.5, 1.5, width, device="cuda")
+    L.fwd()
+    tail = NormLayer(9, width, "bf16", "bf16", "bf16", EPS, residual=False)
+    tail.x, tail.weight = L.x[-9:].clone(), L.weight
+    tail.fwd()
+    assert torch.equal(L.out[-9:], tail.out)
+    L.sum, L.dOut, tail.sum, tail.dOut = L.x, L.out, tail.x, tail.out
+    L.bwd(); tail.bwd()
+    assert torch.equal(L.dX[-9:], tail.dX)
