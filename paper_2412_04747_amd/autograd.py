@@ -3,8 +3,12 @@
 `rgat`, `rgcn` and `hgt` are differentiable functions of torch tensors that live on the GPU;
 `RgatConv`, `RgcnConv` and `HgtConv` are `torch.nn.Module`s holding the parameters.  Forward and
 backward are the C-ABI calls of `binding`; PyTorch only owns the memory, the stream and the
-tape.  Everything is fp32 (the training protocol of the thesis' evaluation section: full-graph
+tape.  The layers are fp32 (the training protocol of the thesis' evaluation section: full-graph
 training of a two-layer model with a negative-log-likelihood loss).
+
+`residual_norm` and `gated_ffn` (`ResidualNorm`, `GatedFfn`) are what stands between the layers of a residual
+model; they take fp32 or bf16 rows and need no graph.  `clip_grad_norm_` bounds the global norm of a model's
+gradients before the optimiser's step.
 
 The workspace of a (layer kind, width, options) combination is allocated once per graph, kept on the
 `Graph` object and dropped by `Graph.close()`; every call of that combination on the graph reuses it,
@@ -13,6 +17,7 @@ so such calls must not overlap on different streams.
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 from .harness import Graph, _buf, _stream
@@ -129,6 +134,145 @@ class _Hgt(torch.autograd.Function):
         return (None, *g, dmu)
 
 
+def _rows(*tensors):
+    """The tensors (None stays) as the row operators take them: contiguous fp32 or bf16, on one GPU."""
+    device = next(t.device for t in tensors if t is not None)
+    for t in tensors:
+        if t is not None and (t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda or t.device != device):
+            raise TypeError("rgnn row operators take fp32 or bf16 CUDA tensors on one device")
+    # (a contiguous slice may still start between 16-byte boundaries)
+    return [t if t is None else t.contiguous() if t.data_ptr() % 16 == 0 or not t.is_contiguous() else t.clone() for t in tensors]
+
+
+def _code(dtype):
+    return B.RGNN_BF16 if dtype == torch.bfloat16 else B.RGNN_F32
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, eps, out_dtype, x, residual, weight):
+        ctx.set_materialize_grads(False)
+        x, residual, weight = _rows(x, residual, weight)
+        width = weight.numel()
+        if weight.dim() != 1 or width == 0 or weight.dtype != torch.float32:
+            raise TypeError("residual_norm: weight is a vector in fp32")
+        if x.dim() < 1 or x.shape[-1] != width or (residual is not None and residual.shape != x.shape):
+            raise ValueError(f"residual_norm: rows of {width} are wanted, got {tuple(x.shape)}"
+                             + (f" and {tuple(residual.shape)}" if residual is not None else ""))
+        with torch.cuda.device(x.device):
+            total = torch.empty_like(residual) if residual is not None else None
+            out = torch.empty(x.shape, dtype=out_dtype, device=x.device)
+            kept = x if total is None else total
+            ctx.desc = B.make_norm_desc(x.numel() // width, width, _code(x.dtype), _code(kept.dtype), _code(out_dtype), eps)
+            B.rgnn_norm_fwd(ctx.desc, x, residual, weight, total, out, _stream())
+        ctx.x_dtype, ctx.residual = x.dtype, residual is not None
+        ctx.save_for_backward(kept, weight)
+        return (out, total) if ctx.residual else out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dOut, dSum=None):
+        kept, weight = ctx.saved_tensors
+        if dOut is None:                   # only the sum was used
+            if dSum is None:
+                return None, None, None, None, None
+            return None, None, dSum.to(ctx.x_dtype), dSum, None
+        dOut, dSum = _rows(dOut, dSum)
+        with torch.cuda.device(kept.device):
+            need_x, need_r, need_w = ctx.needs_input_grad[2:]
+            same = ctx.x_dtype == kept.dtype
+            dX = torch.empty(kept.shape, dtype=ctx.x_dtype, device=kept.device) if need_x or (need_r and same) else None
+            dR = torch.empty_like(kept) if need_r and not same else None
+            dW = torch.empty_like(weight) if need_w else None
+            ws = _buf(B.rgnn_norm_workspace_bytes(ctx.desc)) if need_w else None
+            B.rgnn_norm_bwd(ctx.desc, kept, weight, dOut, dSum, dX, dR, dW, ws, _stream())
+        return None, None, dX if need_x else None, (dX if same else dR) if need_r else None, dW
+
+
+class _GatedFfn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, act, X, Wg, Wu, Wd):
+        X, Wg, Wu, Wd = _rows(X, Wg, Wu, Wd)
+        if Wg.dim() != 2 or X.dim() < 1 or X.shape[-1] != Wg.shape[0] or Wu.shape != Wg.shape or Wd.shape != Wg.shape[::-1]:
+            raise ValueError(f"gated_ffn: shapes {tuple(X.shape)}, {tuple(Wg.shape)}, {tuple(Wu.shape)}, {tuple(Wd.shape)} do not fit")
+        if not X.dtype == Wg.dtype == Wu.dtype == Wd.dtype:
+            raise TypeError("gated_ffn: rows and weights are of one type")
+        width, hidden = Wg.shape
+        with torch.cuda.device(X.device):
+            ctx.desc = B.make_ffn_desc(X.numel() // width, width, hidden, _code(X.dtype),
+                                       {"silu": B.RGNN_ACT_SILU, "relu": B.RGNN_ACT_RELU}[act])
+            out = torch.empty_like(X)
+            B.rgnn_ffn_fwd(ctx.desc, X, Wg, Wu, Wd, out, _buf(B.rgnn_ffn_workspace_bytes(ctx.desc)[0]), _stream())
+        ctx.save_for_backward(X, Wg, Wu, Wd)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dOut):
+        X, Wg, Wu, Wd = ctx.saved_tensors
+        dOut, = _rows(dOut)
+        need_x, *need_w = ctx.needs_input_grad[1:]
+        with torch.cuda.device(X.device):
+            dX = torch.empty_like(X) if need_x else None
+            g = [torch.empty_like(W) if any(need_w) else None for W in (Wg, Wu, Wd)]
+            B.rgnn_ffn_bwd(ctx.desc, X, Wg, Wu, Wd, dOut, dX, *g, _buf(B.rgnn_ffn_workspace_bytes(ctx.desc)[1]), _stream())
+        return (None, dX, *(t if n else None for t, n in zip(g, need_w)))
+
+
+def residual_norm(x, weight, residual=None, eps=1e-6, out_dtype=None):
+    """Residual addition and root-mean-square norm over the last dimension, s = x + residual, out = s / sqrt(mean(s^2) + eps) * weight:
+    (out, s), or out alone without a residual.  s has the residual's type; out has out_dtype (default: x's); weight is fp32."""
+    return _ResidualNorm.apply(float(eps), out_dtype or x.dtype, x, residual, weight)
+
+
+def gated_ffn(X, Wg, Wu, Wd, act="silu"):
+    """Gated feed-forward block (act(X Wg) * (X Wu)) Wd over the last dimension; Wg, Wu [d, hidden], Wd [hidden, d], all of X's type."""
+    if act not in ("silu", "relu"):
+        raise ValueError(f"gated_ffn: unknown activation {act!r}")
+    return _GatedFfn.apply(act, X, Wg, Wu, Wd)
+
+
+def _dense(t):
+    """Whether the tensor's elements fill one stretch of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+@torch.no_grad()
+def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
+    """Scales the gradients of `parameters` in place by min(1, max_norm / (norm + 1e-6)), norm the 2-norm of all of them together, and
+    returns that norm (0-dim fp32 tensor on the GPU; nothing waits for it unless error_if_nonfinite).  Gradients are fp32 or bf16, on one
+    GPU; two that share memory are refused."""
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
+    given = [p.grad for p in parameters if p.grad is not None]
+    if not given:
+        return torch.zeros(())
+    for g in given:
+        if g.layout != torch.strided or g.dtype not in (torch.float32, torch.bfloat16) or not g.is_cuda or g.device != given[0].device:
+            raise TypeError("clip_grad_norm_ takes dense fp32 or bf16 gradients on one GPU")
+    with torch.cuda.device(given[0].device):
+        grads = [g if _dense(g) else g.contiguous() for g in given]
+        sizes = [g.numel() for g in grads]
+        norm = torch.empty((), device=given[0].device)
+        dtypes, ws = [_code(g.dtype) for g in grads], _buf(B.rgnn_clip_workspace_bytes(sizes))
+        if error_if_nonfinite:
+            B.rgnn_clip_grad_norm(grads, None, sizes, dtypes, float(max_norm), norm, ws, _stream())
+            if not torch.isfinite(norm):
+                raise RuntimeError(f"the norm of the gradients is {norm.item()}, so that they cannot be clipped")
+        B.rgnn_clip_grad_norm(grads, grads, sizes, dtypes, float(max_norm), norm, ws, _stream())
+        for g, c in zip(given, grads):
+            if c is not g:
+                g.copy_(c)
+    return norm
+
+
 def rgat(graph, X, W, w_s, w_t, slope=0.2, heads=1):
     """RGAT layer (listing of the single-headed RGAT layer in the thesis; with heads > 1 each head
     works on its slice of the d columns): out [N, d].  On a large graph a call outside grad mode may take another plan
@@ -187,4 +331,27 @@ class HgtConv(torch.nn.Module):
         return hgt(graph, X, self.Wk, self.Wq, self.Wv, self.Wo, self.Watt, self.Wmsg, self.mu)
 
 
-__all__ = ["Graph", "rgat", "rgcn", "hgt", "RgatConv", "RgcnConv", "HgtConv", "release"]
+class ResidualNorm(torch.nn.Module):
+    def __init__(self, width, eps=1e-6, out_dtype=None):
+        super().__init__()
+        self.eps, self.out_dtype = eps, out_dtype
+        self.weight = torch.nn.Parameter(torch.ones(width, device="cuda"))
+
+    def forward(self, x, residual=None):
+        return residual_norm(x, self.weight, residual, self.eps, self.out_dtype)
+
+
+class GatedFfn(torch.nn.Module):
+    def __init__(self, width, hidden, act="silu", dtype=torch.float32):
+        super().__init__()
+        self.act = act
+        p = lambda *shape, fan_in: torch.nn.Parameter(_param(*shape, fan_in=fan_in).detach().to(dtype))
+        self.Wg, self.Wu = p(width, hidden, fan_in=width), p(width, hidden, fan_in=width)
+        self.Wd = p(hidden, width, fan_in=hidden)
+
+    def forward(self, X):
+        return gated_ffn(X, self.Wg, self.Wu, self.Wd, self.act)
+
+
+__all__ = ["Graph", "rgat", "rgcn", "hgt", "RgatConv", "RgcnConv", "HgtConv", "release", "residual_norm", "gated_ffn",
+           "clip_grad_norm_", "ResidualNorm", "GatedFfn"]
