@@ -299,18 +299,31 @@ def train_step_bench(args):
     g = A.Graph(N, R, c["src"], c["dst"], c["rel"])
     torch.manual_seed(synth.SEED0)
     layers = [A.RgatConv(R, d, c["slope"]), A.RgatConv(R, d, c["slope"])]
-    params = [q for l in layers for q in l.parameters()]
+    norms = [A.ResidualNorm(d) for _ in range(5)] if args.block else []
+    ffns = [A.GatedFfn(d, args.block) for _ in range(2)] if args.block else []
+    params = [q for l in layers + norms + ffns for q in l.parameters()]
     X = torch.tensor(c["X"], dtype=torch.float32, device="cuda")
     rng = np.random.default_rng(synth.SEED0)
     train = torch.as_tensor(rng.choice(N, max(N // 10, 1), replace=False), device="cuda")
     labels = torch.as_tensor(rng.integers(0, d, len(train)), device="cuda")
     opt = torch.optim.SGD(params, lr=1e-3)
 
+    def model():
+        if not args.block:
+            return layers[1](g, torch.relu(layers[0](g, X)))
+        y, stream = norms[0](X), X
+        for i in range(2):
+            y, stream = norms[2 * i + 1](layers[i](g, y), stream)
+            y, stream = norms[2 * i + 2](ffns[i](y), stream)
+        return y
+
     def step():
         opt.zero_grad(set_to_none=True)
-        h = layers[1](g, torch.relu(layers[0](g, X)))
+        h = model()
         loss = torch.nn.functional.nll_loss(torch.log_softmax(h[train], dim=1), labels)
         loss.backward()
+        if args.clip_norm:
+            A.clip_grad_norm_(params, args.clip_norm)
         opt.step()
         return loss
 
@@ -332,8 +345,10 @@ def train_step_bench(args):
         "value": 2 * E * args.steps / dt, "unit": "edges/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
         "ms_per_step": dt * 1e3 / args.steps, "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
         "dtype": "f32", "data": "synthetic",
-        "config": {"workload": f"configs[{args.config - 1}] graph, two RGAT layers of width {d}, N={N}, R={R}, E={E}; "
-                               "value counts every edge once per layer"},
+        "config": {"workload": f"configs[{args.config - 1}] graph, two RGAT layers of width {d}, N={N}, R={R}, E={E}"
+                               + (f", each in a residual block with a feed-forward block of hidden width {args.block}" if args.block else "")
+                               + (f", gradients clipped to norm {args.clip_norm:g}" if args.clip_norm else "")
+                               + "; value counts every edge once per layer"},
         "library_kernel_ms_per_step": lib_ms}))
 
 
@@ -365,6 +380,9 @@ def main():
     ap.add_argument("--train", action="store_true",
                     help="time a full training step instead: two RGAT layers through the autograd front end, "
                          "log-softmax + NLL loss on 10%% of the nodes, SGD update (RGAT workloads only)")
+    ap.add_argument("--block", type=int, default=0, metavar="HIDDEN",
+                    help="with --train: each layer in a pre-norm residual block, followed by a gated feed-forward block of that hidden width")
+    ap.add_argument("--clip-norm", type=float, default=0.0, help="with --train: clip the global norm of the gradients before the update")
     args = ap.parse_args()
     if args.gpus != 1:
         sys.exit("bench.py: this build runs on one GPU only (--gpus 1); sharding over several GPUs is a design "
@@ -378,6 +396,8 @@ def main():
     assert torch.cuda.is_available(), "bench.py needs a GPU"
     if args.train:
         return train_step_bench(args)
+    if args.block or args.clip_norm:
+        sys.exit("bench.py --block / --clip-norm: only with --train")
     t0 = time.time()
     c = synth.config(args.config, args.scale)
     if args.dtype:

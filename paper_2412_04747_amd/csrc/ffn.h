@@ -13,6 +13,7 @@ namespace rgnn {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef unsigned rgnn_v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kHid = 32;                 // hidden values of a chunk
 
@@ -108,7 +109,6 @@ struct FfnGradArgs {
     int splits, groups;      // workgroups by rows and by hidden values
 };
 // ffn_grad.hip
-int ffn_grad_group(const rgnn_ffn_desc_t* d);            // hidden values of a workgroup
 int ffn_grad_splits(const rgnn_ffn_desc_t* d);
 rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, void* dWg, void* dWu, void* dWd, hipStream_t st);
 

@@ -19,8 +19,22 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kWaves = 4;
 constexpr int UNIT = 32;
+
+// Hidden values of a wavefront (MT), wavefronts of a workgroup, and wavefronts that share a SIMD.
+template <int D, int PL> struct Cut {
+    static constexpr bool wide = D == 128 && PL == 3;
+    static constexpr int MT = PL == 1 && D < 128 ? 32 : 16;
+    static constexpr int waves = MT == 32 || wide ? 4 : 8;
+    static constexpr int per_simd = wide ? 1 : 2;
+};
+struct Sizes { int group, resident; };       // hidden values of a workgroup; workgroups that fill the GPU's 256 compute units
+template <int D, int PL> constexpr Sizes sizes_of() { return {Cut<D, PL>::MT * Cut<D, PL>::waves, 256 * 4 * Cut<D, PL>::per_simd / Cut<D, PL>::waves}; }
+Sizes sizes(const rgnn_ffn_desc_t* d) {
+    if (d->dtype == RGNN_BF16) return d->width == 32 ? sizes_of<32, 1>() : d->width == 64 ? sizes_of<64, 1>() : sizes_of<128, 1>();
+    return d->width == 32 ? sizes_of<32, 3>() : d->width == 64 ? sizes_of<64, 3>() : sizes_of<128, 3>();
+}
+int groups_of(const rgnn_ffn_desc_t* d) { return (d->hidden + sizes(d).group - 1) / sizes(d).group; }
 
 // 16-byte piece c of row r of a plane sits at piece c ^ swizzle(r): 16 consecutive rows' pieces lie in different places modulo 256 bytes,
 // and so do the pieces of four rows that the transposing read takes together.
@@ -30,22 +44,25 @@ __device__ __forceinline__ int swizzle(int r) {
     return (((r >> L) & (7 >> L)) << 1) | ((r >> 3) & 1);
 }
 
-template <int D, int PL, int ACT, int MT>
-__global__ __launch_bounds__(64 * kWaves, 1) void ffn_grad_kernel(FfnGradArgs k) {
+template <int D, int PL, int ACT>
+__global__ __launch_bounds__((64 * Cut<D, PL>::waves), (Cut<D, PL>::per_simd)) void ffn_grad_kernel(FfnGradArgs k) {
+    constexpr int MT = Cut<D, PL>::MT, WAVES = Cut<D, PL>::waves;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     using Acc = typename std::conditional<MT == 32, v16f, v4f>::type;
     constexpr int KS = MT == 32 ? 16 : 32;               // contraction of an instruction
     constexpr int S = D / KS, NR = MT == 32 ? 16 : 4, RTS = UNIT / MT, STEPS = UNIT / KS, TILES = D / MT;
     constexpr int PLANE = UNIT * D * 2, BUF = 2 * PL * PLANE;
-    constexpr int ITEMS = UNIT * D / 4 / (64 * kWaves);  // pieces of four columns that a thread loads of either tensor
+    // pieces of V columns (16 bytes, or 8 where the unit has fewer than the threads) that a thread loads of either tensor
+    constexpr int V = PL == 3 || UNIT * D / 8 < 64 * WAVES ? 4 : 8, PIECES = UNIT * D / V, ITEMS = (PIECES + 64 * WAVES - 1) / (64 * WAVES);
+    using Raw = typename std::conditional<sizeof(T) * V == 16, rgnn_v4u, rgnn_v2u>::type;
     extern __shared__ unsigned char lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & (MT - 1), kg = lane / MT;
     const FfnArgs& a = k.a;
     // workgroups of one share of the rows are on one chiplet, whose L2 then holds the rows for all of them
     const int split = (int)(blockIdx.x % 8) + 8 * (int)(blockIdx.x / (8 * k.groups)), group = (int)(blockIdx.x / 8) % k.groups;
     if (split >= k.splits) return;
-    const int F = a.hidden, FP = a.chunks * kHid, h = (group * kWaves + wave) * MT + m;
-    const bool mine = (group * kWaves + wave) * MT < FP;
+    const int F = a.hidden, FP = a.chunks * kHid, h = (group * WAVES + wave) * MT + m;
+    const bool mine = (group * WAVES + wave) * MT < FP;
 
     bf16x8 wg[S][PL], wu[S][PL], wd[S][PL];
 #pragma unroll
@@ -72,53 +89,63 @@ __global__ __launch_bounds__(64 * kWaves, 1) void ffn_grad_kernel(FfnGradArgs k)
     }
 
     const int64_t units = (a.rows + UNIT - 1) / UNIT;
-    float xr[ITEMS][4], yr[ITEMS][4];
+    Raw xr[ITEMS], yr[ITEMS];
     auto load = [&](int64_t u) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int at = threadIdx.x + i * 64 * kWaves, rr = at / (D / 4), c = at % (D / 4) * 4;
+            const int at = threadIdx.x + i * 64 * WAVES, rr = at / (D / V), c = at % (D / V) * V;
             const int64_t row = u * UNIT + rr;
-            zero_cols<4>(xr[i]);
-            zero_cols<4>(yr[i]);
-            if (row < a.rows) {
-                load_cols<4>(static_cast<const T*>(a.X) + row * D + c, xr[i]);
-                load_cols<4>(static_cast<const T*>(a.dOut) + row * D + c, yr[i]);
+            xr[i] = yr[i] = Raw{};
+            if (at < PIECES && row < a.rows) {
+                xr[i] = *reinterpret_cast<const Raw*>(static_cast<const T*>(a.X) + row * D + c);
+                yr[i] = *reinterpret_cast<const Raw*>(static_cast<const T*>(a.dOut) + row * D + c);
             }
         }
     };
     auto put = [&](unsigned char* buf) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int at = threadIdx.x + i * 64 * kWaves, rr = at / (D / 4), c = at % (D / 4) * 4;
+            const int at = threadIdx.x + i * 64 * WAVES, rr = at / (D / V), c = at % (D / V) * V;
+            if (PIECES % (64 * WAVES) && at >= PIECES) break;
             unsigned char* const p = buf + rr * (2 * D) + (((c >> 3) ^ swizzle<D>(rr)) << 4) + (c & 4) * 2;
-            const float v[8] = {xr[i][0], xr[i][1], xr[i][2], xr[i][3], yr[i][0], yr[i][1], yr[i][2], yr[i][3]};
-            bf16x8 q[PL];
-            planes8<PL>(v, q);
+            if constexpr (PL == 1) {
+                *reinterpret_cast<Raw*>(p) = xr[i];
+                *reinterpret_cast<Raw*>(p + PLANE) = yr[i];
+            } else {
+                float v[8];
 #pragma unroll
-            for (int l = 0; l < PL; ++l) {
-                const uint4 w = __builtin_bit_cast(uint4, q[l]);
-                *reinterpret_cast<uint2*>(p + l * PLANE) = make_uint2(w.x, w.y);
-                *reinterpret_cast<uint2*>(p + (PL + l) * PLANE) = make_uint2(w.z, w.w);
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = __uint_as_float(xr[i][e]);
+                    v[4 + e] = __uint_as_float(yr[i][e]);
+                }
+                bf16x8 q[PL];
+                planes8<PL>(v, q);
+#pragma unroll
+                for (int l = 0; l < PL; ++l) {
+                    const uint4 w = __builtin_bit_cast(uint4, q[l]);
+                    *reinterpret_cast<uint2*>(p + l * PLANE) = make_uint2(w.x, w.y);
+                    *reinterpret_cast<uint2*>(p + (PL + l) * PLANE) = make_uint2(w.z, w.w);
+                }
             }
         }
     };
+    // A lane's place in the LDS for the first operand of either kind.  The others are XORs and sums of it with constants, as the swizzle
+    // repeats after 16 rows and moves by one piece after 8.
+    const int i16 = lane & 15, half = MT == 32 ? (lane >> 4) & 1 : 0, tr = 4 * kg + (i16 >> 2);
+    const int rows_at = m * (2 * D) + ((kg ^ swizzle<D>(m)) << 4);
+    const int cols_at = (tr & 15) * (2 * D) + (((2 * half + ((i16 & 3) >> 1)) ^ swizzle<D>(tr)) << 4) + (i16 & 1) * 8;
     // rows of tile i, columns KS s + 8 kg ..: of X (which = 0) or dOut (1)
-    auto rows_operand = [&](const unsigned char* buf, int which, int i, int s, bf16x8 (&f)[PL]) {
-        const int r = i * MT + m;
-        const unsigned char* const p = buf + which * PL * PLANE + r * (2 * D) + (((KS / 8 * s + kg) ^ swizzle<D>(r)) << 4);
+    auto rows_operand = [&](const unsigned char* buf, int at, int which, int i, int s, bf16x8 (&f)[PL]) {
+        const unsigned char* const p = buf + ((at ^ (KS * 2 * s)) + i * MT * 2 * D + which * PL * PLANE);
 #pragma unroll
         for (int l = 0; l < PL; ++l) f[l] = *reinterpret_cast<const bf16x8*>(p + l * PLANE);
     };
-    // columns MT t + m, the rows in the order of the accumulators' values 8 s ..
-    const int i16 = lane & 15, half = MT == 32 ? (lane >> 4) & 1 : 0;
-    auto cols_operand = [&](const unsigned char* buf, int which, int t, int s, bf16x8 (&f)[PL]) {
-        const int r0 = (MT == 32 ? 16 * s : 0) + 4 * kg + (i16 >> 2), r1 = r0 + (MT == 32 ? 8 : 16);
-        const int piece = (MT * t + 16 * half) / 8 + ((i16 & 3) >> 1), low = (i16 & 1) * 8;
-        const unsigned char* const b = buf + which * PL * PLANE;
-        const unsigned char* const p = b + r0 * (2 * D) + ((piece ^ swizzle<D>(r0)) << 4) + low;
-        const unsigned char* const q = b + r1 * (2 * D) + ((piece ^ swizzle<D>(r1)) << 4) + low;
+    // columns MT t + m, the rows in the order of the accumulators' values 8 s ..: rows 16 s + 4 kg .. and 8 further, or 4 kg .. and 16 further
+    auto cols_operand = [&](const unsigned char* buf, int at, int which, int t, int s, bf16x8 (&f)[PL]) {
+        const int p = (at ^ (MT * 2 * t)) + s * 16 * 2 * D + which * PL * PLANE;
+        const int q = (at ^ (MT * 2 * t) ^ (MT == 32 ? 16 : 0)) + s * 16 * 2 * D + which * PL * PLANE + (MT == 32 ? 8 : 16) * 2 * D;
 #pragma unroll
-        for (int l = 0; l < PL; ++l) f[l] = tr8(p + l * PLANE, q + l * PLANE);
+        for (int l = 0; l < PL; ++l) f[l] = tr8(buf + p + l * PLANE, buf + q + l * PLANE);
     };
 
     int64_t u = split;
@@ -130,6 +157,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void ffn_grad_kernel(FfnGradArgs k)
         if (u + k.splits < units) load(u + k.splits);
         __syncthreads();         // (a wavefront is at most one unit ahead of another: two buffers are enough)
         if (!mine) continue;
+        int ra = rows_at, ca = cols_at;
+        asm volatile("" : "+v"(ra), "+v"(ca));           // (the places are formed here, not kept across the loop)
         Acc g[RTS], up[RTS], dh[RTS];
 #pragma unroll
         for (int i = 0; i < RTS; ++i) {
@@ -139,10 +168,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void ffn_grad_kernel(FfnGradArgs k)
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 bf16x8 f[PL];
-                rows_operand(buf, 0, i, s, f);
+                rows_operand(buf, ra, 0, i, s, f);
                 mul_add<PL>(f, wg[s], g[i]);
                 mul_add<PL>(f, wu[s], up[i]);
-                rows_operand(buf, 1, i, s, f);
+                rows_operand(buf, ra, 1, i, s, f);
                 mul_add<PL>(f, wd[s], dh[i]);
             }
         }
@@ -170,10 +199,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void ffn_grad_kernel(FfnGradArgs k)
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
                     bf16x8 f[PL];
-                    cols_operand(buf, 0, t, s, f);
+                    cols_operand(buf, ca, 0, t, s, f);
                     mul_add<PL>(f, gp[s], dwg[t]);
                     mul_add<PL>(f, upp[s], dwu[t]);
-                    cols_operand(buf, 1, t, s, f);
+                    cols_operand(buf, ca, 1, t, s, f);
                     mul_add<PL>(f, hp[s], dwd[t]);
                 }
             } else {
@@ -184,10 +213,10 @@ __global__ __launch_bounds__(64 * kWaves, 1) void ffn_grad_kernel(FfnGradArgs k)
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
                     bf16x8 f[PL];
-                    cols_operand(buf, 0, t, s, f);
+                    cols_operand(buf, ca, 0, t, s, f);
                     mul_add<PL>(f, gp[s], tg);
                     mul_add<PL>(f, upp[s], tu);
-                    cols_operand(buf, 1, t, s, f);
+                    cols_operand(buf, ca, 1, t, s, f);
                     mul_add<PL>(f, hp[s], td);
                 }
 #pragma unroll
@@ -228,27 +257,22 @@ __global__ __launch_bounds__(256) void ffn_grad_reduce_kernel(const float* part,
 
 }  // namespace
 
-static int tile_of(const rgnn_ffn_desc_t* d) { return d->dtype == RGNN_F32 && d->width == 128 ? 16 : 32; }
-int ffn_grad_group(const rgnn_ffn_desc_t* d) { return kWaves * tile_of(d); }
-// As many shares as make one workgroup per compute unit (two where both fit), a multiple of 8 for the chiplets; no more than units.
+// As many shares as fill the GPU once, a multiple of 8 for the chiplets; no more than units.
 int ffn_grad_splits(const rgnn_ffn_desc_t* d) {
     const int64_t units = (d->rows + UNIT - 1) / UNIT;
-    const int groups = (d->hidden + ffn_grad_group(d) - 1) / ffn_grad_group(d);
-    const int64_t want = std::max(8, 512 / groups / 8 * 8);
-    return (int)std::min(want, units);
+    return (int)std::min<int64_t>(std::max(8, sizes(d).resident / groups_of(d) / 8 * 8), units);
 }
 
 rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, void* dWg, void* dWu, void* dWd, hipStream_t st) {
-    FfnGradArgs k{a, part, ffn_grad_splits(d), (d->hidden + ffn_grad_group(d) - 1) / ffn_grad_group(d)};
+    FfnGradArgs k{a, part, ffn_grad_splits(d), groups_of(d)};
     if (k.splits > 0) {
         auto run = [&]() -> rgnn_status_t {
             RGNN_DISPATCH_FFN(d, {
-                constexpr int MT = PL == 3 && D == 128 ? 16 : 32;
                 constexpr size_t lds = 2 * 2 * PL * UNIT * D * 2;
-                auto* const kernel = ffn_grad_kernel<D, PL, ACT, MT>;
+                auto* const kernel = ffn_grad_kernel<D, PL, ACT>;
                 RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
                 KernelTimer timer(st, "ffn_bwd_weights");
-                kernel<<<(unsigned)((k.splits + 7) / 8 * 8 * k.groups), 64 * kWaves, lds, st>>>(k);
+                kernel<<<(unsigned)((k.splits + 7) / 8 * 8 * k.groups), 64 * Cut<D, PL>::waves, lds, st>>>(k);
                 RGNN_CHECK_LAUNCH();
                 return RGNN_OK;
             });
