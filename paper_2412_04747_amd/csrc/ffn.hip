@@ -60,12 +60,17 @@ __global__ __launch_bounds__(256) void ffn_pack_kernel(PackArgs a) {
     for (int k = 0; k < PL; ++k) *reinterpret_cast<bf16x8*>(to + k * kFrag) = p[k];
 }
 
-// n operands from memory into the LDS, by all wavefronts of the workgroup
-__device__ __forceinline__ void fetch(const unsigned char* from, unsigned char* lds, int n) {
-    const int lane = threadIdx.x & 63;
-    for (int k = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); k < n; k += kWaves)
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (size_t)k * kFrag + lane * 16),
-                                         (__attribute__((address_space(3))) void*)(lds + k * kFrag), 16, 0, 0);
+// N operands from memory into the LDS, by all wavefronts of the workgroup
+template <int N>
+__device__ __forceinline__ void fetch(const unsigned char* from, unsigned char* lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < (N + kWaves - 1) / kWaves; ++i) {
+        const int k = i * kWaves + wave;
+        if (N % kWaves == 0 || k < N)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (size_t)k * kFrag + lane * 16),
+                                             (__attribute__((address_space(3))) void*)(lds + k * kFrag), 16, 0, 0);
+    }
 }
 // what this wavefront has under way has arrived, then all have
 __device__ __forceinline__ void arrived() {
@@ -113,99 +118,162 @@ __device__ __forceinline__ void store_result(const RowsArgs& r, int64_t row, int
         }
 }
 
-template <int D, int PL, int ACT, int RT, bool BWD>
-__global__ __launch_bounds__(64 * kWaves, 1) void ffn_rows_kernel(RowsArgs r) {
-    constexpr int S = D / 16, TILES = D / 32, OPS = S * PL, FIRST = (BWD ? 3 : 2) * OPS, SECOND = (BWD ? 2 : 1) * OPS;
+// Hidden values of a chunk while they are formed: gate, up and (backward) the gradient of their product.
+template <bool BWD> struct Hidden { v16f g, u; };
+template <> struct Hidden<true> { v16f g, u, dh; };
+
+// What a chunk's weights take in the LDS.  One plane: twice, so that one barrier per chunk is enough; three planes (up to 120 KB, and six
+// times the instructions to wait behind): once, the halves of a chunk refilled in turn.
+template <int D, int PL, bool BWD> struct Weights {
+    static constexpr int ops = D / 16 * PL, first = (BWD ? 3 : 2) * ops, second = (BWD ? 2 : 1) * ops;
+    static constexpr bool twice = PL == 1;
+    static constexpr size_t lds = (size_t)(first + second) * kFrag * (twice ? 2 : 1);
+};
+
+// The products of chunk c + 1 are issued between the activations of chunk c: the matrix unit and the vector unit work at the same time
+// within a wavefront.
+template <int D, int PL, int ACT, bool BWD>
+__global__ __launch_bounds__(64 * kWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kernel(RowsArgs r) {
+    using W = Weights<D, PL, BWD>;
+    constexpr int S = D / 16, TILES = D / 32;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     extern __shared__ unsigned char lds[];
-    unsigned char* const first = lds;
-    unsigned char* const second = lds + FIRST * kFrag;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
-    const int64_t row0 = ((int64_t)blockIdx.x * kWaves + wave) * (32 * RT) + m;
+    const int64_t row = ((int64_t)blockIdx.x * kWaves + wave) * 32 + m;
     const int c0 = (int)((int64_t)r.a.chunks * blockIdx.y / r.splits), c1 = (int)((int64_t)r.a.chunks * (blockIdx.y + 1) / r.splits);
-    const unsigned char* from = r.packed + (size_t)c0 * (FIRST + SECOND) * kFrag;
-    fetch(from, first, FIRST);
+    auto first = [&](int c) { return lds + (W::twice ? (c & 1) * (W::first + W::second) * kFrag : 0); };
+    auto second = [&](int c) { return first(c) + W::first * kFrag; };
+    auto fetch_first = [&](int c) { if (c < c1) fetch<W::first>(r.packed + (size_t)c * (W::first + W::second) * kFrag, first(c)); };
+    auto fetch_second = [&](int c) { if (c < c1) fetch<W::second>(r.packed + ((size_t)c * (W::first + W::second) + W::first) * kFrag, second(c)); };
+    fetch_first(c0);
+    if (W::twice) {
+        fetch_first(c0 + 1);
+        fetch_second(c0);
+    }
+    bf16x8 x[S][PL], dy[BWD ? S : 1][PL];
+    v16f y[TILES];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        load_planes8<PL>(static_cast<const T*>(r.a.X) + row * D + 16 * s + 8 * kh, row < r.a.rows, x[s]);
+        if constexpr (BWD) load_planes8<PL>(static_cast<const T*>(r.a.dOut) + row * D + 16 * s + 8 * kh, row < r.a.rows, dy[s]);
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) clear(y[t]);
 
-    bf16x8 x[RT][S][PL], dy[BWD ? RT : 1][BWD ? S : 1][PL];
-    v16f y[RT][TILES];
+    // Operands are read from the LDS a step before they are multiplied.  The compiler would move the reads to their use and wait there; the
+    // backward, whose registers are full, is left to it (2M rows, d 128, f 512, bf16, forward: 935 us without the fences, 913 with;
+    // 200017 rows, f 341, backward: 119 and 134).
+    auto fence = [] { if constexpr (!BWD) __builtin_amdgcn_sched_barrier(0); };
+    struct FirstOps { bf16x8 f[BWD ? 3 : 2][PL]; };
+    struct SecondOps { bf16x8 f[BWD ? 2 : 1][PL]; };
+    auto read_first = [&](const unsigned char* w, int s) {
+        FirstOps o;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int64_t row = row0 + 32 * i;
-        const bool ok = row < r.a.rows;
+        for (int k = 0; k < (BWD ? 3 : 2); ++k) operand(w + (k * S + s) * PL * kFrag, o.f[k]);
+        return o;
+    };
+    auto read_second = [&](const unsigned char* w, int q) {           // q = TILES s + t
+        SecondOps o;
 #pragma unroll
-        for (int s = 0; s < S; ++s) {
-            load_planes8<PL>(static_cast<const T*>(r.a.X) + row * D + 16 * s + 8 * kh, ok, x[i][s]);
-            if constexpr (BWD) load_planes8<PL>(static_cast<const T*>(r.a.dOut) + row * D + 16 * s + 8 * kh, ok, dy[i][s]);
-        }
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) clear(y[i][t]);
-    }
-    for (int c = c0; c < c1; ++c, from += (size_t)(FIRST + SECOND) * kFrag) {
+        for (int k = 0; k < (BWD ? 2 : 1); ++k) operand(w + (k * S + 2 * (q % TILES) + q / TILES) * PL * kFrag, o.f[k]);
+        return o;
+    };
+    // the s-th sixteen columns' share of the chunk's hidden values
+    auto form = [&](const FirstOps& o, int s, Hidden<BWD>& h) {
+        mul_add<PL>(o.f[0], x[s], h.g);
+        mul_add<PL>(o.f[1], x[s], h.u);
+        if constexpr (BWD) mul_add<PL>(o.f[2], dy[s], h.dh);
+    };
+    auto none = [&](Hidden<BWD>& h) {
+        clear(h.g);
+        clear(h.u);
+        if constexpr (BWD) clear(h.dh);
+    };
+    auto chunk = [&](auto more, int c, Hidden<BWD>& now, Hidden<BWD>& next) {      // more: there is a chunk c + 1
         arrived();
-        fetch(from + (size_t)FIRST * kFrag, second, SECOND);
-        v16f g[RT], u[RT], dh[BWD ? RT : 1];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            clear(g[i]);
-            clear(u[i]);
-            if constexpr (BWD) clear(dh[i]);
+        if (W::twice) {
+            fetch_first(c + 2);
+            fetch_second(c + 1);
+        } else {
+            fetch_second(c);
         }
-#pragma unroll
-        for (int s = 0; s < S; ++s) {
-            bf16x8 wg[PL], wu[PL];
-            operand(first + s * PL * kFrag, wg);
-            operand(first + (S + s) * PL * kFrag, wu);
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                mul_add<PL>(wg, x[i][s], g[i]);
-                mul_add<PL>(wu, x[i][s], u[i]);
-            }
+        float v[16], v2[BWD ? 16 : 1];
+        auto activate = [&](int j) {
             if constexpr (BWD) {
-                bf16x8 wd[PL];
-                operand(first + (2 * S + s) * PL * kFrag, wd);
-#pragma unroll
-                for (int i = 0; i < RT; ++i) mul_add<PL>(wd, dy[i][s], dh[i]);
+                float a, slope;
+                act_slope<ACT>(now.g[j], a, slope);
+                v[j] = now.dh[j] * now.u[j] * slope;
+                v2[j] = now.dh[j] * a;
+            } else {
+                v[j] = act<ACT>(now.g[j]) * now.u[j];
             }
+        };
+        if constexpr (more()) {
+            none(next);
+            FirstOps o = read_first(first(c + 1), 0);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                FirstOps ahead;
+                if (s + 1 < S) ahead = read_first(first(c + 1), s + 1);
+                fence();
+                form(o, s, next);
+#pragma unroll
+                for (int j = 0; j < 16 / S; ++j) activate(16 / S * s + j);
+                fence();
+                o = ahead;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) activate(j);
         }
-        arrived();
-        if (c + 1 < c1) fetch(from + (size_t)(FIRST + SECOND) * kFrag, first, FIRST);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            bf16x8 p[RT][PL], p2[BWD ? RT : 1][PL];
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                float v[8], v2[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float gv = g[i][8 * s + j], uv = u[i][8 * s + j];
-                    if constexpr (BWD) {
-                        float av, slope;
-                        act_slope<ACT>(gv, av, slope);
-                        v[j] = dh[i][8 * s + j] * uv * slope;
-                        v2[j] = dh[i][8 * s + j] * av;
-                    } else {
-                        v[j] = act<ACT>(gv) * uv;
-                    }
-                }
-                planes8<PL>(v, p[i]);
-                if constexpr (BWD) planes8<PL>(v2, p2[i]);
-            }
-#pragma unroll
-            for (int t = 0; t < TILES; ++t) {
-                bf16x8 w[PL];
-                operand(second + (2 * t + s) * PL * kFrag, w);
-#pragma unroll
-                for (int i = 0; i < RT; ++i) mul_add<PL>(w, p[i], y[i][t]);
-                if constexpr (BWD) {
-                    operand(second + (S + 2 * t + s) * PL * kFrag, w);
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) mul_add<PL>(w, p2[i], y[i][t]);
-                }
-            }
+        if (!W::twice) {
+            arrived();
+            fetch_first(c + 2);
         }
+        SecondOps o = read_second(second(c), 0);
+        bf16x8 p[2][PL], p2[2][PL];
+        auto round = [&](int s) {
+            planes8<PL>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
+            if constexpr (BWD) planes8<PL>(*reinterpret_cast<const float(*)[8]>(v2 + 8 * s), p2[s]);
+        };
+        round(0);
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+            SecondOps ahead;
+            if (q + 1 < S) ahead = read_second(second(c), q + 1);
+            fence();
+            const int s = q / TILES, t = q % TILES;
+            mul_add<PL>(o.f[0], p[s], y[t]);
+            if constexpr (BWD) mul_add<PL>(o.f[1], p2[s], y[t]);
+            if (q == 0) round(1);
+            fence();
+            o = ahead;
+        }
+    };
+    Hidden<BWD> a, b;
+    none(a);
+    arrived();
+#pragma unroll
+    for (int s = 0; s < S; ++s) form(read_first(first(c0), s), s, a);
+    if (!W::twice) {
+        __syncthreads();
+        fetch_first(c0 + 1);
     }
-#pragma unroll
-    for (int i = 0; i < RT; ++i) store_result<D, PL>(r, row0 + 32 * i, kh, y[i]);
+    // (two at a time: the sets of hidden values change places without being moved)
+    constexpr std::true_type more;
+    constexpr std::false_type last;
+    int c = c0;
+    for (; c + 2 < c1; c += 2) {
+        chunk(more, c, a, b);
+        chunk(more, c + 1, b, a);
+    }
+    if (c + 1 < c1) {
+        chunk(more, c, a, b);
+        chunk(last, c + 1, b, a);
+    } else {
+        chunk(last, c, a, b);
+    }
+    store_result<D, PL>(r, row, kh, y);
 }
 
 // The splits' shares, added in order.  Four columns per thread.
@@ -230,32 +298,30 @@ __global__ __launch_bounds__(256) void ffn_combine_kernel(const float* part, int
 }
 
 int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
-// Wavefronts take 32 rows, or 64 where the operands of 64 fit their registers: the weights then cross the LDS half as often.
-int row_tiles(const rgnn_ffn_desc_t* d, bool) { return d->dtype == RGNN_BF16 && d->rows >= 65536 ? 2 : 1; }
+constexpr int kBlockRows = 32 * kWaves;
 // One workgroup per compute unit at least, as far as the chunks go.
-int splits_of(const rgnn_ffn_desc_t* d, bool backward) {
-    const int64_t blocks = (d->rows + 32 * kWaves * row_tiles(d, backward) - 1) / (32 * kWaves * row_tiles(d, backward));
+int splits_of(const rgnn_ffn_desc_t* d) {
+    const int64_t blocks = (d->rows + kBlockRows - 1) / kBlockRows;
     return blocks >= 256 || blocks == 0 ? 1 : (int)std::min<int64_t>(chunks_of(d), (256 + blocks - 1) / blocks);
 }
 size_t packed_bytes(const rgnn_ffn_desc_t* d, bool backward) {
     return align_up((size_t)chunks_of(d) * (backward ? 5 : 3) * (d->width / 16) * (d->dtype == RGNN_BF16 ? 1 : 3) * kFrag);
 }
-size_t share_bytes(const rgnn_ffn_desc_t* d, bool backward) {
-    const int s = splits_of(d, backward);
+size_t share_bytes(const rgnn_ffn_desc_t* d) {
+    const int s = splits_of(d);
     return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
 }
 size_t grad_bytes(const rgnn_ffn_desc_t* d) {
     return align_up(sizeof(float) * (size_t)ffn_grad_splits(d) * 3 * d->width * chunks_of(d) * kHid);
 }
 
-template <int D, int PL, int ACT, int RT, bool BWD>
+template <int D, int PL, int ACT, bool BWD>
 rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
-    constexpr size_t lds = (size_t)(BWD ? 5 : 3) * (D / 16) * PL * kFrag;
-    auto* const kernel = ffn_rows_kernel<D, PL, ACT, RT, BWD>;
+    constexpr size_t lds = Weights<D, PL, BWD>::lds;
+    auto* const kernel = ffn_rows_kernel<D, PL, ACT, BWD>;
     RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
-    const int64_t per = 32 * kWaves * RT;
     KernelTimer timer(st, BWD ? "ffn_bwd_rows" : "ffn_fwd");
-    kernel<<<dim3((unsigned)((r.a.rows + per - 1) / per), r.splits), 64 * kWaves, lds, st>>>(r);
+    kernel<<<dim3((unsigned)((r.a.rows + kBlockRows - 1) / kBlockRows), r.splits), 64 * kWaves, lds, st>>>(r);
     RGNN_CHECK_LAUNCH();
     return RGNN_OK;
 }
@@ -263,7 +329,7 @@ rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
 template <bool BWD>
 rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, int accumulate, void* workspace, hipStream_t st) {
     unsigned char* const packed = static_cast<unsigned char*>(workspace);
-    const RowsArgs r{a, packed, out, reinterpret_cast<float*>(packed + packed_bytes(d, BWD)), splits_of(d, BWD), accumulate};
+    const RowsArgs r{a, packed, out, reinterpret_cast<float*>(packed + packed_bytes(d, BWD)), splits_of(d), accumulate};
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
             {
@@ -273,10 +339,7 @@ rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, i
                 ffn_pack_kernel<D, PL><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(p);
                 RGNN_CHECK_LAUNCH();
             }
-            if constexpr (PL == 1) {
-                if (row_tiles(d, BWD) == 2) return launch_rows<D, PL, ACT, 2, BWD>(r, st);
-            }
-            return launch_rows<D, PL, ACT, 1, BWD>(r, st);
+            return launch_rows<D, PL, ACT, BWD>(r, st);
         });
     };
     RGNN_TRY(run());
@@ -325,8 +388,8 @@ using namespace rgnn;
 
 extern "C" rgnn_status_t rgnn_ffn_workspace_bytes(const rgnn_ffn_desc_t* desc, size_t* fwd_workspace, size_t* bwd_workspace) {
     RGNN_TRY(check_desc(desc));
-    if (fwd_workspace) *fwd_workspace = packed_bytes(desc, false) + share_bytes(desc, false);
-    if (bwd_workspace) *bwd_workspace = std::max(packed_bytes(desc, true) + share_bytes(desc, true), grad_bytes(desc));
+    if (fwd_workspace) *fwd_workspace = packed_bytes(desc, false) + share_bytes(desc);
+    if (bwd_workspace) *bwd_workspace = std::max(packed_bytes(desc, true) + share_bytes(desc), grad_bytes(desc));
     return RGNN_OK;
 }
 
@@ -339,7 +402,7 @@ extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X
     const size_t n = (size_t)desc->rows * desc->width, w = (size_t)desc->hidden * desc->width;
     const int32_t t = desc->dtype;
     RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t)},
-                           {span(out, n, t), Span{static_cast<char*>(workspace), packed_bytes(desc, false) + share_bytes(desc, false)}}));
+                           {span(out, n, t), Span{static_cast<char*>(workspace), packed_bytes(desc, false) + share_bytes(desc)}}));
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, nullptr};
     return rows_pass<false>(desc, a, out, 0, workspace, static_cast<hipStream_t>(stream));
 }
