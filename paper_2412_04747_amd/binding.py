@@ -79,6 +79,13 @@ class Schedule(C.Structure):
         return {k: int(getattr(self, k)) for k, _ in self._fields_}
 
 
+# Argument types of the operators on rows, whose calls are short: addresses then go through as plain ints.
+_P = C.c_void_p
+_ROW_OPS = {"rgnn_norm_workspace_bytes": [_P] * 2, "rgnn_norm_fwd": [_P] * 7, "rgnn_norm_bwd": [_P] * 10,
+            "rgnn_ffn_workspace_bytes": [_P] * 3, "rgnn_ffn_fwd": [_P] * 8, "rgnn_ffn_bwd": [_P] * 12,
+            "rgnn_clip_workspace_bytes": [C.c_int64, _P, _P],
+            "rgnn_clip_grad_norm": [C.c_int64, _P, _P, _P, _P, C.c_float, _P, _P, _P]}
+
 _lib = None
 
 
@@ -92,6 +99,8 @@ def lib():
         _lib.rgnn_last_error.restype = C.c_char_p
         for name in EXPORTS[1:]:
             getattr(_lib, name).restype = C.c_int
+        for name, types in _ROW_OPS.items():
+            getattr(_lib, name).argtypes = types
     return _lib
 
 
@@ -203,13 +212,18 @@ def rgnn_norm_workspace_bytes(desc):
     return b.value
 
 
+def _addr(x):
+    """Address of a torch tensor, or the int or None itself."""
+    return x if x is None or type(x) is int else x.data_ptr()
+
+
 def rgnn_norm_fwd(desc, x, residual, weight, sum, out, stream=None):
-    _check(lib().rgnn_norm_fwd(C.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum), _ptr(out), _ptr(stream)))
+    _check(lib().rgnn_norm_fwd(C.byref(desc), _addr(x), _addr(residual), _addr(weight), _addr(sum), _addr(out), stream))
 
 
 def rgnn_norm_bwd(desc, sum, weight, dOut, dSum, dX, dResidual, dWeight, workspace, stream=None):
-    _check(lib().rgnn_norm_bwd(C.byref(desc), _ptr(sum), _ptr(weight), _ptr(dOut), _ptr(dSum), _ptr(dX), _ptr(dResidual),
-                               _ptr(dWeight), _ptr(workspace), _ptr(stream)))
+    _check(lib().rgnn_norm_bwd(C.byref(desc), _addr(sum), _addr(weight), _addr(dOut), _addr(dSum), _addr(dX), _addr(dResidual),
+                               _addr(dWeight), _addr(workspace), stream))
 
 
 def make_ffn_desc(rows, width, hidden, dtype=RGNN_F32, activation=RGNN_ACT_SILU, flags=0):
@@ -224,27 +238,28 @@ def rgnn_ffn_workspace_bytes(desc):
 
 
 def rgnn_ffn_fwd(desc, X, Wg, Wu, Wd, out, workspace, stream=None):
-    _check(lib().rgnn_ffn_fwd(C.byref(desc), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(out), _ptr(workspace), _ptr(stream)))
+    _check(lib().rgnn_ffn_fwd(C.byref(desc), _addr(X), _addr(Wg), _addr(Wu), _addr(Wd), _addr(out), _addr(workspace), stream))
 
 
 def rgnn_ffn_bwd(desc, X, Wg, Wu, Wd, dOut, dX, dWg, dWu, dWd, workspace, stream=None):
-    _check(lib().rgnn_ffn_bwd(C.byref(desc), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(dOut), _ptr(dX), _ptr(dWg), _ptr(dWu),
-                              _ptr(dWd), _ptr(workspace), _ptr(stream)))
+    _check(lib().rgnn_ffn_bwd(C.byref(desc), _addr(X), _addr(Wg), _addr(Wu), _addr(Wd), _addr(dOut), _addr(dX), _addr(dWg), _addr(dWu),
+                              _addr(dWd), _addr(workspace), stream))
 
 
 def rgnn_clip_workspace_bytes(sizes):
     b = C.c_size_t()
     n = len(sizes)
-    _check(lib().rgnn_clip_workspace_bytes(C.c_int64(n), (C.c_int64 * n)(*sizes), C.byref(b)))
+    _check(lib().rgnn_clip_workspace_bytes(n, (C.c_int64 * n)(*sizes), C.byref(b)))
     return b.value
 
 
 def rgnn_clip_grad_norm(grads, clipped, sizes, dtypes, max_norm, norm, workspace, stream=None):
     """grads, clipped: lists of torch tensors or raw pointers; clipped may be None (the norm alone)."""
     n = len(grads)
-    addr = lambda ts: (C.c_void_p * n)(*[t if isinstance(t, int) or t is None else t.data_ptr() for t in ts])
-    _check(lib().rgnn_clip_grad_norm(C.c_int64(n), addr(grads), None if clipped is None else addr(clipped), (C.c_int64 * n)(*sizes),
-                                     (C.c_int32 * n)(*dtypes), C.c_float(max_norm), _ptr(norm), _ptr(workspace), _ptr(stream)))
+    given = (_P * n)(*map(_addr, grads))
+    results = None if clipped is None else given if clipped is grads else (_P * n)(*map(_addr, clipped))
+    _check(lib().rgnn_clip_grad_norm(n, given, results, (C.c_int64 * n)(*sizes), (C.c_int32 * n)(*dtypes), max_norm, _addr(norm),
+                                     _addr(workspace), stream))
 
 
 def rgnn_profile_select(name=None):

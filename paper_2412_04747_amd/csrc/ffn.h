@@ -87,30 +87,144 @@ __device__ __forceinline__ void act_slope(float g, float& a, float& slope) {
     slope = s + a * (1.f - s);
 }
 
-// Eight consecutive columns of a row, as planes; zeros where !ok.
-template <int PL, typename T>
-__device__ __forceinline__ void load_planes8(const T* p, bool ok, bf16x8 (&f)[PL]) {
+// Eight consecutive columns, 16 s + 8 kh and on, of row min(row, rows - 1) as planes; zeros past the last row.  (The load itself is not a
+// branch's: a wavefront would wait for each of its loads by itself.)
+template <int D, int PL, typename T>
+__device__ __forceinline__ void load_planes8(const T* X, int64_t row, int64_t rows, int col, bf16x8 (&f)[PL]) {
+    const bool ok = row < rows;
+    const T* const p = X + (ok ? row : rows - 1) * D + col;
     if constexpr (PL == 1) {
         static_assert(sizeof(T) == 2, "one plane: bfloat16 storage");
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (ok) v = *reinterpret_cast<const uint4*>(p);
-        f[0] = __builtin_bit_cast(bf16x8, v);
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        f[0] = __builtin_bit_cast(bf16x8, make_uint4(ok ? v.x : 0, ok ? v.y : 0, ok ? v.z : 0, ok ? v.w : 0));
     } else {
         float v[8];
-        zero_cols<8>(v);
-        if (ok) load_cols<8>(p, v);
+        load_cols<8>(p, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = ok ? v[e] : 0.f;
         planes8<PL>(v, f);
     }
 }
 
-struct FfnGradArgs {
+constexpr int kRowWaves = 4;             // wavefronts of a workgroup in the passes of the rows, 32 rows each
+constexpr int kFrag = 1024;              // bytes of an operand of a wavefront's instruction
+
+// Sections of a chunk's weights, each D / 16 operands of PL planes.
+enum { kGate, kUp, kDown, kOut, kGateBack, kUpBack };
+__host__ __device__ constexpr int section(bool backward, int i) { return !backward || i < 2 ? i : i == 2 ? kOut : i == 3 ? kGateBack : kUpBack; }
+
+// A lane's eight values of operand s of a section, from the weights as they are given; zeros past the last hidden value.
+template <int D, int PL, int WHAT>
+__device__ __forceinline__ void weight_values(const FfnArgs& a, int chunk, int s, int lane, float (&v)[8]) {
+    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
+    const int m = lane & 31, kh = lane >> 5, F = a.hidden;
+    const T* const W = static_cast<const T*>(WHAT == kGate || WHAT == kGateBack ? a.Wg : WHAT == kUp || WHAT == kUpBack ? a.Wu : a.Wd);
+    if constexpr (WHAT == kOut) {        // eight columns of a row of Wd
+        const int h = chunk * kHid + m;
+        load_cols<8>(W + (size_t)min(h, F - 1) * D + 16 * s + 8 * kh, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = h < F ? v[j] : 0.f;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            // hidden value, column of the row: 16 s + 8 kh + j of hidden value m; or columns 32 (s / 2) + m, the (s % 2)-th 16 hidden values in
+            // the order of an accumulator
+            const int h = chunk * kHid + (WHAT == kGate || WHAT == kUp ? m : 16 * (s & 1) + 8 * (j >> 2) + 4 * kh + (j & 3));
+            const int c = WHAT == kGate || WHAT == kUp ? 16 * s + 8 * kh + j : 32 * (s >> 1) + m;
+            const int at = min(h, F - 1);
+            v[j] = widen(W[WHAT == kDown ? (size_t)at * D + c : (size_t)c * F + at]);
+            v[j] = h < F ? v[j] : 0.f;
+        }
+    }
+}
+
+template <int PL>
+__device__ __forceinline__ void operand(const unsigned char* at, bf16x8 (&f)[PL]) {
+#pragma unroll
+    for (int k = 0; k < PL; ++k) f[k] = *reinterpret_cast<const bf16x8*>(at + k * kFrag + (threadIdx.x & 63) * 16);
+}
+
+struct RowsArgs {
     FfnArgs a;
-    float* part;             // [splits][3][D][chunks * kHid]: dWg, dWu and dWd transposed
-    int splits, groups;      // workgroups by rows and by hidden values
+    const unsigned char* packed;
+    void* out;               // rows of the result
+    float* part;             // with several splits: [splits][rows][D]
+    int splits, accumulate;
 };
+
+// The lane's row of the result: tile t holds columns 32 t + 8 q + 4 kh + (0..3) in values 4 q .. 4 q + 3.
+template <int D, int PL>
+__device__ __forceinline__ void store_result(const RowsArgs& r, int split, int64_t row, int kh, const v16f (&y)[D / 32]) {
+    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
+    if (row >= r.a.rows) return;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float v[4] = {y[t][4 * q], y[t][4 * q + 1], y[t][4 * q + 2], y[t][4 * q + 3]};
+            const int64_t at = row * D + 32 * t + 8 * q + 4 * kh;
+            if (r.splits > 1) {
+                store_cols<4>(r.part + (int64_t)split * r.a.rows * D + at, v);
+            } else {
+                T* const p = static_cast<T*>(r.out) + at;
+                if (r.accumulate) {
+                    float o[4];
+                    load_cols<4>(p, o);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += o[e];
+                }
+                store_cols<4>(p, v);
+            }
+        }
+}
+
+// Hidden values of a chunk while they are formed: gate, up and (backward) the gradient of their product.
+template <bool BWD> struct Hidden { v16f g, u; };
+template <> struct Hidden<true> { v16f g, u, dh; };
+
+// Value j of act(g) u; backward: of dg and du.
+template <int ACT>
+__device__ __forceinline__ void activate(const Hidden<false>& h, int j, float& v, float&) { v = act<ACT>(h.g[j]) * h.u[j]; }
+template <int ACT>
+__device__ __forceinline__ void activate(const Hidden<true>& h, int j, float& v, float& v2) {
+    float a, slope;
+    act_slope<ACT>(h.g[j], a, slope);
+    v = h.dh[j] * h.u[j] * slope;
+    v2 = h.dh[j] * a;
+}
+
+// The splits' shares of n elements, added in order.  Four columns per thread.
+template <typename T>
+__device__ __forceinline__ void combine_block(const float* part, int splits, int64_t n, T* out, int accumulate, int block) {
+    const int64_t i = ((int64_t)block * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    float sum[4];
+    zero_cols<4>(sum);
+#pragma unroll 4
+    for (int k = 0; k < splits; ++k) {
+        float v[4];
+        load_cols<4>(part + k * n + i, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += v[e];
+    }
+    if (accumulate) {
+        float o[4];
+        load_cols<4>(out + i, o);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += o[e];
+    }
+    store_cols<4>(out + i, sum);
+}
+
 // ffn_grad.hip
 int ffn_grad_splits(const rgnn_ffn_desc_t* d);
 rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, void* dWg, void* dWu, void* dWd, hipStream_t st);
+
+// ffn_few.hip: the same for few rows
+bool ffn_few(const rgnn_ffn_desc_t* d);
+size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward);
+rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st);
+rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st);
 
 #define RGNN_DISPATCH_FFN(DESC, ...)                                                                                   \
     do {                                                                                                               \

@@ -17,47 +17,32 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kFrag = 1024;              // bytes of an operand of a wavefront's instruction
-
-// Sections of a chunk, each D / 16 operands of PL planes.  Forward: gate, up, down.  Backward: gate, up, out, gate back, up back.
-enum { kGate, kUp, kDown, kOut, kGateBack, kUpBack };
-
-// One lane's eight values of an operand.
-struct PackArgs { int hidden, chunks, backward; const void* Wg; const void* Wu; const void* Wd; unsigned char* to; };
+// The weights of all chunks as operands.
+struct PackArgs { FfnArgs a; int backward; unsigned char* to; };
 template <int D, int PL>
-__global__ __launch_bounds__(256) void ffn_pack_kernel(PackArgs a) {
+__global__ __launch_bounds__(256) void ffn_pack_kernel(PackArgs p) {
     constexpr int S = D / 16;
-    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
-    const int sections = a.backward ? 5 : 3;
+    const int sections = p.backward ? 5 : 3;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int lane = (int)(id & 63), s = (int)((id >> 6) % S);
     const int64_t q = (id >> 6) / S;
     const int sec = (int)(q % sections);
     const int64_t chunk = q / sections;
-    if (chunk >= a.chunks) return;
-    const int what = a.backward ? (sec == 2 ? kOut : sec == 3 ? kGateBack : sec == 4 ? kUpBack : sec) : sec;
-    const int m = lane & 31, kh = lane >> 5, F = a.hidden;
-    const T* W = static_cast<const T*>(what == kGate || what == kGateBack ? a.Wg : what == kUp || what == kUpBack ? a.Wu : a.Wd);
+    if (chunk >= p.a.chunks) return;
     float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        int h, c;                        // hidden value, column of the row
-        if (what == kGate || what == kUp || what == kOut) {
-            h = (int)chunk * kHid + m;
-            c = 16 * s + 8 * kh + j;
-        } else {                         // operand s: columns 32 (s / 2) + m, the (s % 2)-th 16 hidden values in the order of an accumulator
-            h = (int)chunk * kHid + 16 * (s & 1) + 8 * (j >> 2) + 4 * kh + (j & 3);
-            c = 32 * (s >> 1) + m;
-        }
-        const bool down = what == kDown || what == kOut;
-        v[j] = h < F ? widen(W[down ? (size_t)h * D + c : (size_t)c * F + h]) : 0.f;
+    switch (section(p.backward, sec)) {
+        case kGate: weight_values<D, PL, kGate>(p.a, (int)chunk, s, lane, v); break;
+        case kUp: weight_values<D, PL, kUp>(p.a, (int)chunk, s, lane, v); break;
+        case kDown: weight_values<D, PL, kDown>(p.a, (int)chunk, s, lane, v); break;
+        case kOut: weight_values<D, PL, kOut>(p.a, (int)chunk, s, lane, v); break;
+        case kGateBack: weight_values<D, PL, kGateBack>(p.a, (int)chunk, s, lane, v); break;
+        default: weight_values<D, PL, kUpBack>(p.a, (int)chunk, s, lane, v);
     }
-    bf16x8 p[PL];
-    planes8<PL>(v, p);
-    unsigned char* const to = a.to + (((chunk * sections + sec) * S + s) * PL) * kFrag + lane * 16;
+    bf16x8 f[PL];
+    planes8<PL>(v, f);
+    unsigned char* const to = p.to + (((chunk * sections + sec) * S + s) * PL) * kFrag + lane * 16;
 #pragma unroll
-    for (int k = 0; k < PL; ++k) *reinterpret_cast<bf16x8*>(to + k * kFrag) = p[k];
+    for (int k = 0; k < PL; ++k) *reinterpret_cast<bf16x8*>(to + k * kFrag) = f[k];
 }
 
 // N operands from memory into the LDS, by all wavefronts of the workgroup
@@ -65,9 +50,9 @@ template <int N>
 __device__ __forceinline__ void fetch(const unsigned char* from, unsigned char* lds) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < (N + kWaves - 1) / kWaves; ++i) {
-        const int k = i * kWaves + wave;
-        if (N % kWaves == 0 || k < N)
+    for (int i = 0; i < (N + kRowWaves - 1) / kRowWaves; ++i) {
+        const int k = i * kRowWaves + wave;
+        if (N % kRowWaves == 0 || k < N)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (size_t)k * kFrag + lane * 16),
                                              (__attribute__((address_space(3))) void*)(lds + k * kFrag), 16, 0, 0);
     }
@@ -77,50 +62,6 @@ __device__ __forceinline__ void arrived() {
     __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
     __syncthreads();
 }
-
-template <int PL>
-__device__ __forceinline__ void operand(const unsigned char* at, bf16x8 (&f)[PL]) {
-#pragma unroll
-    for (int k = 0; k < PL; ++k) f[k] = *reinterpret_cast<const bf16x8*>(at + k * kFrag + (threadIdx.x & 63) * 16);
-}
-
-struct RowsArgs {
-    FfnArgs a;
-    const unsigned char* packed;
-    void* out;               // rows of the result
-    float* part;             // with several splits: [splits][rows][D]
-    int splits, accumulate;
-};
-
-// The lane's row of the result: tile t holds columns 32 t + 8 q + 4 kh + (0..3) in values 4 q .. 4 q + 3.
-template <int D, int PL>
-__device__ __forceinline__ void store_result(const RowsArgs& r, int64_t row, int kh, const v16f (&y)[D / 32]) {
-    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
-    if (row >= r.a.rows) return;
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            float v[4] = {y[t][4 * q], y[t][4 * q + 1], y[t][4 * q + 2], y[t][4 * q + 3]};
-            const int64_t at = row * D + 32 * t + 8 * q + 4 * kh;
-            if (r.splits > 1) {
-                store_cols<4>(r.part + (int64_t)blockIdx.y * r.a.rows * D + at, v);
-            } else {
-                T* const p = static_cast<T*>(r.out) + at;
-                if (r.accumulate) {
-                    float o[4];
-                    load_cols<4>(p, o);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] += o[e];
-                }
-                store_cols<4>(p, v);
-            }
-        }
-}
-
-// Hidden values of a chunk while they are formed: gate, up and (backward) the gradient of their product.
-template <bool BWD> struct Hidden { v16f g, u; };
-template <> struct Hidden<true> { v16f g, u, dh; };
 
 // What a chunk's weights take in the LDS.  One plane: twice, so that one barrier per chunk is enough; three planes (up to 120 KB, and six
 // times the instructions to wait behind): once, the halves of a chunk refilled in turn.
@@ -133,13 +74,13 @@ template <int D, int PL, bool BWD> struct Weights {
 // The products of chunk c + 1 are issued between the activations of chunk c: the matrix unit and the vector unit work at the same time
 // within a wavefront.
 template <int D, int PL, int ACT, bool BWD>
-__global__ __launch_bounds__(64 * kWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kernel(RowsArgs r) {
+__global__ __launch_bounds__(64 * kRowWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kernel(RowsArgs r) {
     using W = Weights<D, PL, BWD>;
     constexpr int S = D / 16, TILES = D / 32;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     extern __shared__ unsigned char lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
-    const int64_t row = ((int64_t)blockIdx.x * kWaves + wave) * 32 + m;
+    const int64_t row = ((int64_t)blockIdx.x * kRowWaves + wave) * 32 + m;
     const int c0 = (int)((int64_t)r.a.chunks * blockIdx.y / r.splits), c1 = (int)((int64_t)r.a.chunks * (blockIdx.y + 1) / r.splits);
     auto first = [&](int c) { return lds + (W::twice ? (c & 1) * (W::first + W::second) * kFrag : 0); };
     auto second = [&](int c) { return first(c) + W::first * kFrag; };
@@ -154,8 +95,8 @@ __global__ __launch_bounds__(64 * kWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kerne
     v16f y[TILES];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        load_planes8<PL>(static_cast<const T*>(r.a.X) + row * D + 16 * s + 8 * kh, row < r.a.rows, x[s]);
-        if constexpr (BWD) load_planes8<PL>(static_cast<const T*>(r.a.dOut) + row * D + 16 * s + 8 * kh, row < r.a.rows, dy[s]);
+        load_planes8<D, PL>(static_cast<const T*>(r.a.X), row, r.a.rows, 16 * s + 8 * kh, x[s]);
+        if constexpr (BWD) load_planes8<D, PL>(static_cast<const T*>(r.a.dOut), row, r.a.rows, 16 * s + 8 * kh, dy[s]);
     }
 #pragma unroll
     for (int t = 0; t < TILES; ++t) clear(y[t]);
@@ -197,17 +138,7 @@ __global__ __launch_bounds__(64 * kWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kerne
         } else {
             fetch_second(c);
         }
-        float v[16], v2[BWD ? 16 : 1];
-        auto activate = [&](int j) {
-            if constexpr (BWD) {
-                float a, slope;
-                act_slope<ACT>(now.g[j], a, slope);
-                v[j] = now.dh[j] * now.u[j] * slope;
-                v2[j] = now.dh[j] * a;
-            } else {
-                v[j] = act<ACT>(now.g[j]) * now.u[j];
-            }
-        };
+        float v[16], v2[16];
         if constexpr (more()) {
             none(next);
             FirstOps o = read_first(first(c + 1), 0);
@@ -218,13 +149,13 @@ __global__ __launch_bounds__(64 * kWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kerne
                 fence();
                 form(o, s, next);
 #pragma unroll
-                for (int j = 0; j < 16 / S; ++j) activate(16 / S * s + j);
+                for (int j = 0; j < 16 / S; ++j) activate<ACT>(now, 16 / S * s + j, v[16 / S * s + j], v2[16 / S * s + j]);
                 fence();
                 o = ahead;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) activate(j);
+            for (int j = 0; j < 16; ++j) activate<ACT>(now, j, v[j], v2[j]);
         }
         if (!W::twice) {
             arrived();
@@ -273,32 +204,16 @@ __global__ __launch_bounds__(64 * kWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kerne
     } else {
         chunk(last, c, a, b);
     }
-    store_result<D, PL>(r, row, kh, y);
+    store_result<D, PL>(r, blockIdx.y, row, kh, y);
 }
 
-// The splits' shares, added in order.  Four columns per thread.
 template <typename T>
 __global__ __launch_bounds__(256) void ffn_combine_kernel(const float* part, int splits, int64_t n, T* out, int accumulate) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    float s[4];
-    zero_cols<4>(s);
-    if (accumulate) load_cols<4>(out + i, s);
-    float sum[4];
-    zero_cols<4>(sum);
-    for (int k = 0; k < splits; ++k) {
-        float v[4];
-        load_cols<4>(part + k * n + i, v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += v[e];
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[e] += sum[e];
-    store_cols<4>(out + i, s);
+    combine_block(part, splits, n, out, accumulate, blockIdx.x);
 }
 
 int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
-constexpr int kBlockRows = 32 * kWaves;
+constexpr int kBlockRows = 32 * kRowWaves;
 // One workgroup per compute unit at least, as far as the chunks go.
 int splits_of(const rgnn_ffn_desc_t* d) {
     const int64_t blocks = (d->rows + kBlockRows - 1) / kBlockRows;
@@ -315,13 +230,19 @@ size_t grad_bytes(const rgnn_ffn_desc_t* d) {
     return align_up(sizeof(float) * (size_t)ffn_grad_splits(d) * 3 * d->width * chunks_of(d) * kHid);
 }
 
+size_t workspace_bytes(const rgnn_ffn_desc_t* d, bool backward) {
+    if (ffn_few(d)) return ffn_few_bytes(d, backward);
+    const size_t rows = packed_bytes(d, backward) + share_bytes(d);
+    return backward ? std::max(rows, grad_bytes(d)) : rows;
+}
+
 template <int D, int PL, int ACT, bool BWD>
 rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
     constexpr size_t lds = Weights<D, PL, BWD>::lds;
     auto* const kernel = ffn_rows_kernel<D, PL, ACT, BWD>;
     RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
     KernelTimer timer(st, BWD ? "ffn_bwd_rows" : "ffn_fwd");
-    kernel<<<dim3((unsigned)((r.a.rows + kBlockRows - 1) / kBlockRows), r.splits), 64 * kWaves, lds, st>>>(r);
+    kernel<<<dim3((unsigned)((r.a.rows + kBlockRows - 1) / kBlockRows), r.splits), 64 * kRowWaves, lds, st>>>(r);
     RGNN_CHECK_LAUNCH();
     return RGNN_OK;
 }
@@ -333,7 +254,7 @@ rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, i
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
             {
-                const PackArgs p{a.hidden, a.chunks, BWD, a.Wg, a.Wu, a.Wd, packed};
+                const PackArgs p{a, BWD, packed};
                 const int64_t threads = (int64_t)a.chunks * (BWD ? 5 : 3) * (D / 16) * 64;
                 KernelTimer timer(st, "ffn_pack");
                 ffn_pack_kernel<D, PL><<<(unsigned)((threads + 255) / 256), 256, 0, st>>>(p);
@@ -388,8 +309,8 @@ using namespace rgnn;
 
 extern "C" rgnn_status_t rgnn_ffn_workspace_bytes(const rgnn_ffn_desc_t* desc, size_t* fwd_workspace, size_t* bwd_workspace) {
     RGNN_TRY(check_desc(desc));
-    if (fwd_workspace) *fwd_workspace = packed_bytes(desc, false) + share_bytes(desc);
-    if (bwd_workspace) *bwd_workspace = std::max(packed_bytes(desc, true) + share_bytes(desc), grad_bytes(desc));
+    if (fwd_workspace) *fwd_workspace = workspace_bytes(desc, false);
+    if (bwd_workspace) *bwd_workspace = workspace_bytes(desc, true);
     return RGNN_OK;
 }
 
@@ -402,9 +323,10 @@ extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X
     const size_t n = (size_t)desc->rows * desc->width, w = (size_t)desc->hidden * desc->width;
     const int32_t t = desc->dtype;
     RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t)},
-                           {span(out, n, t), Span{static_cast<char*>(workspace), packed_bytes(desc, false) + share_bytes(desc)}}));
+                           {span(out, n, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, false)}}));
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, nullptr};
-    return rows_pass<false>(desc, a, out, 0, workspace, static_cast<hipStream_t>(stream));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return ffn_few(desc) ? ffn_few_fwd(desc, a, out, workspace, st) : rows_pass<false>(desc, a, out, 0, workspace, st);
 }
 
 extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
@@ -417,13 +339,12 @@ extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X
     if (!workspace) RGNN_FAIL(RGNN_EWORKSPACE, "workspace is NULL");
     const size_t n = (size_t)desc->rows * desc->width, w = (size_t)desc->hidden * desc->width;
     const int32_t t = desc->dtype;
-    size_t bytes = 0;
-    RGNN_TRY(rgnn_ffn_workspace_bytes(desc, nullptr, &bytes));
     RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t), span(dOut, n, t)},
-                           {span(dX, n, t), span(dWg, w, t), span(dWu, w, t), span(dWd, w, t), Span{static_cast<char*>(workspace), bytes}}));
+                           {span(dX, n, t), span(dWg, w, t), span(dWu, w, t), span(dWd, w, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, true)}}));
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, dOut};
     const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
+    if (desc->rows > 0 && ffn_few(desc)) return ffn_few_bwd(desc, a, dX, dWg, dWu, dWd, workspace, st);
     if (dX && desc->rows > 0) RGNN_TRY(rows_pass<true>(desc, a, dX, accumulate, workspace, st));
     if (grads && (desc->rows > 0 || !accumulate)) RGNN_TRY(ffn_grad(desc, a, static_cast<float*>(workspace), dWg, dWu, dWd, st));
     return RGNN_OK;

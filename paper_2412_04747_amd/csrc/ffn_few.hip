@@ -1,0 +1,219 @@
+// Gated feed-forward block for few rows, where launches and their latency are the time.
+//
+// The weights are read as they are given and put into the LDS as operands by the workgroups that use them, so that no launch lays them out first;
+// the backward's two passes share a launch, some of its workgroups forming dX and the others the weights' gradients; and what several
+// workgroups add up is summed by one launch for both.  A call is two launches, or one where nothing is divided, against three (forward) and five.
+// Every 128 rows read all weights again: worth it up to kRows rows (see ffn_few).
+#include <math.h>
+
+#include "rgnn_internal.h"
+#include "device_utils.h"
+#include "ffn_grad.h"
+
+namespace rgnn {
+
+namespace {
+
+constexpr int kBlockRows = 32 * kRowWaves;
+
+template <int D, int PL, bool BWD> constexpr int rows_lds() { return (BWD ? 5 : 3) * (D / 16) * PL * kFrag; }
+
+// 128 rows, a share of the chunks.
+template <int D, int PL, int ACT, bool BWD>
+__device__ __forceinline__ void rows_block(const RowsArgs& r, int block, int split, unsigned char* lds) {
+    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves;
+    using T = typename std::conditional<PL == 1, bf16_t, float>::type;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
+    const int64_t row0 = ((int64_t)block * kRowWaves + wave) * 32, row = row0 + m;
+    const int c0 = (int)((int64_t)r.a.chunks * split / r.splits), c1 = (int)((int64_t)r.a.chunks * (split + 1) / r.splits);
+    bf16x8 x[S][PL], dy[BWD ? S : 1][PL];
+    v16f y[TILES];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+        load_planes8<D, PL>(static_cast<const T*>(r.a.X), row, r.a.rows, 16 * s + 8 * kh, x[s]);
+        if constexpr (BWD) load_planes8<D, PL>(static_cast<const T*>(r.a.dOut), row, r.a.rows, 16 * s + 8 * kh, dy[s]);
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) clear(y[t]);
+    for (int c = c0; c < c1; ++c) {
+        // all loads, then all conversions: the wavefronts wait for memory once per chunk
+        float v[SECTIONS][EACH][8];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int s = i * kRowWaves + wave;
+            if (S % kRowWaves && s >= S) break;
+            weight_values<D, PL, section(BWD, 0)>(r.a, c, s, lane, v[0][i]);
+            weight_values<D, PL, section(BWD, 1)>(r.a, c, s, lane, v[1][i]);
+            weight_values<D, PL, section(BWD, 2)>(r.a, c, s, lane, v[2][i]);
+            if constexpr (BWD) {
+                weight_values<D, PL, section(BWD, 3)>(r.a, c, s, lane, v[3][i]);
+                weight_values<D, PL, section(BWD, 4)>(r.a, c, s, lane, v[4][i]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (c > c0) __syncthreads();
+#pragma unroll
+        for (int k = 0; k < SECTIONS; ++k)
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int s = i * kRowWaves + wave;
+                if (S % kRowWaves && s >= S) break;
+                bf16x8 f[PL];
+                planes8<PL>(v[k][i], f);
+#pragma unroll
+                for (int l = 0; l < PL; ++l) *reinterpret_cast<bf16x8*>(lds + ((k * S + s) * PL + l) * kFrag + lane * 16) = f[l];
+            }
+        __syncthreads();
+        if (row0 >= r.a.rows) continue;
+        Hidden<BWD> h;
+        clear(h.g);
+        clear(h.u);
+        if constexpr (BWD) clear(h.dh);
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            bf16x8 f[PL];
+            operand(lds + s * PL * kFrag, f);
+            mul_add<PL>(f, x[s], h.g);
+            operand(lds + (S + s) * PL * kFrag, f);
+            mul_add<PL>(f, x[s], h.u);
+            if constexpr (BWD) {
+                operand(lds + (2 * S + s) * PL * kFrag, f);
+                mul_add<PL>(f, dy[s], h.dh);
+            }
+        }
+        const unsigned char* const w = lds + (BWD ? 3 : 2) * S * PL * kFrag;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            float v[8], v2[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) activate<ACT>(h, 8 * s + j, v[j], v2[j]);
+            bf16x8 p[PL], p2[PL], f[PL];
+            planes8<PL>(v, p);
+            if constexpr (BWD) planes8<PL>(v2, p2);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                operand(w + (2 * t + s) * PL * kFrag, f);
+                mul_add<PL>(f, p, y[t]);
+                if constexpr (BWD) {
+                    operand(w + (S + 2 * t + s) * PL * kFrag, f);
+                    mul_add<PL>(f, p2, y[t]);
+                }
+            }
+        }
+    }
+    store_result<D, PL>(r, split, row, kh, y);
+}
+
+template <int D, int PL, int ACT>
+__global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_fwd_kernel(RowsArgs r) {
+    extern __shared__ unsigned char lds[];
+    rows_block<D, PL, ACT, false>(r, blockIdx.x, blockIdx.y, lds);
+}
+
+// Workgroups [0, row_blocks * r.splits) form dX, the others the weights' gradients.
+template <int D, int PL, int ACT>
+__global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_bwd_kernel(RowsArgs r, FfnGradArgs k, int row_blocks) {
+    extern __shared__ unsigned char lds[];
+    const int b = blockIdx.x, n = row_blocks * r.splits;
+    if (b < n) {
+        rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
+    } else if (k.splits == 1) {
+        grad_block<D, PL, ACT, kRowWaves, true>(k, 0, b - n, lds);
+    } else {
+        grad_block<D, PL, ACT, kRowWaves, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
+    }
+}
+
+// Workgroups [0, row_blocks): the shares of the rows; the others: of the weights' gradients.
+template <typename T>
+__global__ __launch_bounds__(256) void ffn_few_sum_kernel(RowsArgs r, FfnGradArgs k, int D, int row_blocks) {
+    __shared__ float lds[16][64];
+    const int b = blockIdx.x;
+    if (b < row_blocks) combine_block(r.part, r.splits, r.a.rows * D, static_cast<T*>(r.out), r.accumulate, b);
+    else grad_reduce_block<T>(k, D, b - row_blocks, lds);
+}
+
+int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
+int row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 1) / kBlockRows); }
+// Chunks are divided as long as that puts a workgroup more on each compute unit, kept together by kTogether.
+constexpr int kTogether = 2;
+int row_splits(const rgnn_ffn_desc_t* d) {
+    const int most = (chunks_of(d) + kTogether - 1) / kTogether;
+    return std::max(1, std::min(most, 256 / std::max(row_blocks(d), 1)));
+}
+int grad_group(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }
+int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + grad_group(d) - 1) / grad_group(d); }
+// Units of 32 rows: one or two need no division.
+int grad_splits(const rgnn_ffn_desc_t* d) {
+    const int units = (int)((d->rows + UNIT - 1) / UNIT);
+    return units <= 2 ? 1 : std::max(1, std::min(units, 256 / grad_groups(d)));
+}
+size_t share_bytes(const rgnn_ffn_desc_t* d) {
+    const int s = row_splits(d);
+    return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
+}
+size_t grad_bytes(const rgnn_ffn_desc_t* d) {
+    const int s = grad_splits(d);
+    return s > 1 ? align_up(sizeof(float) * (size_t)s * 3 * d->width * chunks_of(d) * kHid) : 0;
+}
+
+rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs& k, hipStream_t st) {
+    const unsigned rows = r.splits > 1 ? (unsigned)((d->rows * d->width / 4 + 255) / 256) : 0;
+    const unsigned grads = k.splits > 1 ? (unsigned)((int64_t)3 * d->width * chunks_of(d) * kHid / 64) : 0;
+    if (rows + grads == 0) return RGNN_OK;
+    KernelTimer timer(st, "ffn_few.sum");
+    if (d->dtype == RGNN_BF16) ffn_few_sum_kernel<bf16_t><<<rows + grads, 256, 0, st>>>(r, k, d->width, (int)rows);
+    else ffn_few_sum_kernel<float><<<rows + grads, 256, 0, st>>>(r, k, d->width, (int)rows);
+    RGNN_CHECK_LAUNCH();
+    return RGNN_OK;
+}
+
+}  // namespace
+
+constexpr int64_t kRows = 4096;
+bool ffn_few(const rgnn_ffn_desc_t* d) { return d->rows <= kRows; }
+size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d) + (backward ? grad_bytes(d) : 0)); }
+
+rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st) {
+    const RowsArgs r{a, nullptr, out, static_cast<float*>(workspace), row_splits(d), 0};
+    auto run = [&]() -> rgnn_status_t {
+        RGNN_DISPATCH_FFN(d, {
+            constexpr int lds = rows_lds<D, PL, false>();
+            auto* const kernel = ffn_few_fwd_kernel<D, PL, ACT>;
+            RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
+            KernelTimer timer(st, "ffn_few_fwd");
+            kernel<<<dim3(row_blocks(d), r.splits), 64 * kRowWaves, lds, st>>>(r);
+            RGNN_CHECK_LAUNCH();
+            return RGNN_OK;
+        });
+    };
+    RGNN_TRY(run());
+    FfnGradArgs k{};
+    k.splits = 1;
+    return sum(d, r, k, st);
+}
+
+rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st) {
+    const int accumulate = (d->flags & RGNN_FLAG_ACCUMULATE) != 0;
+    RowsArgs r{a, nullptr, dX, static_cast<float*>(workspace), row_splits(d), accumulate};
+    FfnGradArgs k{a, reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d)), grad_splits(d), grad_groups(d), dWg, dWu, dWd, accumulate};
+    const int rows = dX ? row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
+    if (rows + grads == 0) return RGNN_OK;
+    auto run = [&]() -> rgnn_status_t {
+        RGNN_DISPATCH_FFN(d, {
+            constexpr int lds = std::max(rows_lds<D, PL, true>(), Cut<D, PL>::lds);
+            auto* const kernel = ffn_few_bwd_kernel<D, PL, ACT>;
+            RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
+            KernelTimer timer(st, "ffn_few_bwd");
+            kernel<<<rows * r.splits + grads, 64 * kRowWaves, lds, st>>>(r, k, rows);
+            RGNN_CHECK_LAUNCH();
+            return RGNN_OK;
+        });
+    };
+    RGNN_TRY(run());
+    if (!rows) r.splits = 1;
+    if (!grads) k.splits = 1;
+    return sum(d, r, k, st);
+}
+
+}  // namespace rgnn
