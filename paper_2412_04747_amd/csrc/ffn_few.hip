@@ -135,11 +135,10 @@ __global__ __launch_bounds__(256) void ffn_few_sum_kernel(RowsArgs r, FfnGradArg
 
 int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
 int row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 1) / kBlockRows); }
-// Chunks are divided as long as that puts a workgroup more on each compute unit, kept together by kTogether.
-constexpr int kTogether = 2;
+// A chunk takes a workgroup 3 to 5 us, most of it latency, the launch that adds the shares 4: three chunks stay together, more are divided
+// as long as that puts a workgroup more on each compute unit.
 int row_splits(const rgnn_ffn_desc_t* d) {
-    const int most = (chunks_of(d) + kTogether - 1) / kTogether;
-    return std::max(1, std::min(most, 256 / std::max(row_blocks(d), 1)));
+    return chunks_of(d) <= 3 ? 1 : std::max(1, std::min(chunks_of(d), 256 / std::max(row_blocks(d), 1)));
 }
 int grad_group(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }
 int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + grad_group(d) - 1) / grad_group(d); }
