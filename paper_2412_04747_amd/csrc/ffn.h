@@ -221,7 +221,7 @@ int ffn_grad_splits(const rgnn_ffn_desc_t* d);
 rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, void* dWg, void* dWu, void* dWd, hipStream_t st);
 
 // ffn_few.hip: the same for few rows
-bool ffn_few(const rgnn_ffn_desc_t* d);
+bool ffn_few(const rgnn_ffn_desc_t* d, bool backward);
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward);
 rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st);
 rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st);

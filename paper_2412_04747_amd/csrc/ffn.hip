@@ -6,7 +6,7 @@
 // order in which the instructions read them (as planes, padded with zeros to whole chunks), come through the LDS for the four
 // wavefronts of a workgroup in two halves that take turns: while one is multiplied the other is on its way.
 // Nothing of the hidden width is written.  Matrix instructions bound it: 6 (10) N d f operations, sixfold for fp32.
-// With few rows the chunks are divided among workgroups too, and a last launch adds their shares in order.
+// (Few rows: ffn_few.hip.)
 #include <math.h>
 
 #include "rgnn_internal.h"
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * kRowWaves, (PL == 1 ? 2 : 1)) void ffn_rows_ke
     extern __shared__ unsigned char lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
     const int64_t row = ((int64_t)blockIdx.x * kRowWaves + wave) * 32 + m;
-    const int c0 = (int)((int64_t)r.a.chunks * blockIdx.y / r.splits), c1 = (int)((int64_t)r.a.chunks * (blockIdx.y + 1) / r.splits);
+    const int c0 = 0, c1 = r.a.chunks;
     auto first = [&](int c) { return lds + (W::twice ? (c & 1) * (W::first + W::second) * kFrag : 0); };
     auto second = [&](int c) { return first(c) + W::first * kFrag; };
     auto fetch_first = [&](int c) { if (c < c1) fetch<W::first>(r.packed + (size_t)c * (W::first + W::second) * kFrag, first(c)); };
@@ -204,36 +204,21 @@ __global__ __launch_bounds__(64 * kRowWaves, (PL == 1 ? 2 : 1)) void ffn_rows_ke
     } else {
         chunk(last, c, a, b);
     }
-    store_result<D, PL>(r, blockIdx.y, row, kh, y);
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void ffn_combine_kernel(const float* part, int splits, int64_t n, T* out, int accumulate) {
-    combine_block(part, splits, n, out, accumulate, blockIdx.x);
+    store_result<D, PL>(r, 0, row, kh, y);
 }
 
 int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
 constexpr int kBlockRows = 32 * kRowWaves;
-// One workgroup per compute unit at least, as far as the chunks go.
-int splits_of(const rgnn_ffn_desc_t* d) {
-    const int64_t blocks = (d->rows + kBlockRows - 1) / kBlockRows;
-    return blocks >= 256 || blocks == 0 ? 1 : (int)std::min<int64_t>(chunks_of(d), (256 + blocks - 1) / blocks);
-}
 size_t packed_bytes(const rgnn_ffn_desc_t* d, bool backward) {
     return align_up((size_t)chunks_of(d) * (backward ? 5 : 3) * (d->width / 16) * (d->dtype == RGNN_BF16 ? 1 : 3) * kFrag);
-}
-size_t share_bytes(const rgnn_ffn_desc_t* d) {
-    const int s = splits_of(d);
-    return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
 }
 size_t grad_bytes(const rgnn_ffn_desc_t* d) {
     return align_up(sizeof(float) * (size_t)ffn_grad_splits(d) * 3 * d->width * chunks_of(d) * kHid);
 }
 
 size_t workspace_bytes(const rgnn_ffn_desc_t* d, bool backward) {
-    if (ffn_few(d)) return ffn_few_bytes(d, backward);
-    const size_t rows = packed_bytes(d, backward) + share_bytes(d);
-    return backward ? std::max(rows, grad_bytes(d)) : rows;
+    if (ffn_few(d, backward)) return ffn_few_bytes(d, backward);
+    return backward ? std::max(packed_bytes(d, true), grad_bytes(d)) : packed_bytes(d, false);
 }
 
 template <int D, int PL, int ACT, bool BWD>
@@ -242,7 +227,7 @@ rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
     auto* const kernel = ffn_rows_kernel<D, PL, ACT, BWD>;
     RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
     KernelTimer timer(st, BWD ? "ffn_bwd_rows" : "ffn_fwd");
-    kernel<<<dim3((unsigned)((r.a.rows + kBlockRows - 1) / kBlockRows), r.splits), 64 * kRowWaves, lds, st>>>(r);
+    kernel<<<(unsigned)((r.a.rows + kBlockRows - 1) / kBlockRows), 64 * kRowWaves, lds, st>>>(r);
     RGNN_CHECK_LAUNCH();
     return RGNN_OK;
 }
@@ -250,7 +235,7 @@ rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
 template <bool BWD>
 rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, int accumulate, void* workspace, hipStream_t st) {
     unsigned char* const packed = static_cast<unsigned char*>(workspace);
-    const RowsArgs r{a, packed, out, reinterpret_cast<float*>(packed + packed_bytes(d, BWD)), splits_of(d), accumulate};
+    const RowsArgs r{a, packed, out, nullptr, 1, accumulate};
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
             {
@@ -263,16 +248,7 @@ rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, i
             return launch_rows<D, PL, ACT, BWD>(r, st);
         });
     };
-    RGNN_TRY(run());
-    if (r.splits > 1) {
-        const int64_t n = a.rows * d->width;
-        KernelTimer timer(st, "ffn_combine");
-        const unsigned blocks = (unsigned)((n / 4 + 255) / 256);
-        if (d->dtype == RGNN_BF16) ffn_combine_kernel<<<blocks, 256, 0, st>>>(r.part, r.splits, n, static_cast<bf16_t*>(out), accumulate);
-        else ffn_combine_kernel<<<blocks, 256, 0, st>>>(r.part, r.splits, n, static_cast<float*>(out), accumulate);
-        RGNN_CHECK_LAUNCH();
-    }
-    return RGNN_OK;
+    return run();
 }
 
 rgnn_status_t check_desc(const rgnn_ffn_desc_t* d) {
@@ -326,7 +302,7 @@ extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X
                            {span(out, n, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, false)}}));
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, nullptr};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return ffn_few(desc) ? ffn_few_fwd(desc, a, out, workspace, st) : rows_pass<false>(desc, a, out, 0, workspace, st);
+    return ffn_few(desc, false) ? ffn_few_fwd(desc, a, out, workspace, st) : rows_pass<false>(desc, a, out, 0, workspace, st);
 }
 
 extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
@@ -344,7 +320,7 @@ extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, dOut};
     const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
-    if (desc->rows > 0 && ffn_few(desc)) return ffn_few_bwd(desc, a, dX, dWg, dWu, dWd, workspace, st);
+    if (desc->rows > 0 && ffn_few(desc, true)) return ffn_few_bwd(desc, a, dX, dWg, dWu, dWd, workspace, st);
     if (dX && desc->rows > 0) RGNN_TRY(rows_pass<true>(desc, a, dX, accumulate, workspace, st));
     if (grads && (desc->rows > 0 || !accumulate)) RGNN_TRY(ffn_grad(desc, a, static_cast<float*>(workspace), dWg, dWu, dWd, st));
     return RGNN_OK;

@@ -3,7 +3,7 @@
 // The weights are read as they are given and put into the LDS as operands by the workgroups that use them, so that no launch lays them out first;
 // the backward's two passes share a launch, some of its workgroups forming dX and the others the weights' gradients; and what several
 // workgroups add up is summed by one launch for both.  A call is two launches, or one where nothing is divided, against three (forward) and five.
-// Every 128 rows read all weights again: worth it up to kRows rows (see ffn_few).
+// Every 128 rows read and split all weights again, which is worth it up to some number of rows (ffn_few).
 #include <math.h>
 
 #include "rgnn_internal.h"
@@ -169,8 +169,18 @@ rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs
 
 }  // namespace
 
-constexpr int64_t kRows = 4096;
-bool ffn_few(const rgnn_ffn_desc_t* d) { return d->rows <= kRows; }
+// Up to which number of rows this is faster than laying out the weights first and taking every pass by itself, in us here / there:
+//   forward   d 32, f 64, bf16: 32000 rows 4.9 / 5.7, 48000 5.5 / 6.3; fp32: 32000 7.8 / 9.3, 48000 11.0 / 11.3
+//             d 64, f 256, bf16: 2000 8.4 / 9.5, 4000 10.4 / 9.6; fp32: 16000 21.9 / 22.4, 24000 25.7 / 22.8
+//             d 128, f 341, bf16: 2000 14.0 / 14.6, 4000 17.8 / 14.7; fp32: 16000 43.9 / 46.5, 24000 56.8 / 47.8
+//   backward  d 32, f 64, bf16: 32000 15.3 / 22.8; fp32: 32000 19.7 / 26.7
+//             d 64, f 256, bf16: 12000 36.2 / 41.6, 24000 50.3 / 42.1; fp32: 16000 57.9 / 61.8, 24000 84.9 / 67.9
+//             d 128, f 341, bf16: 8000 42.4 / 54.3, 12000 57.1 / 55.5; fp32: 16000 138 / 152, 24000 207 / 181
+bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
+    if (d->width == 32) return d->rows <= 32768;
+    if (d->dtype == RGNN_F32) return d->rows <= 16384;
+    return d->rows <= (backward ? 12288 : 2560);
+}
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d) + (backward ? grad_bytes(d) : 0)); }
 
 rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st) {
