@@ -71,25 +71,31 @@ template <int D, int PL, bool BWD> struct Weights {
     static constexpr size_t lds = (size_t)(first + second) * kFrag * (twice ? 2 : 1);
 };
 
-// The products of chunk c + 1 are issued between the activations of chunk c: the matrix unit and the vector unit work at the same time
-// within a wavefront.
+// Wavefronts that share a SIMD, and whether the products of chunk c + 1 are issued between the activations of chunk c (the matrix unit and
+// the vector unit then work at the same time within a wavefront, which takes the registers of a second set of hidden values).
+template <int D, int PL, bool BWD> struct RowsCut {
+    static constexpr int per_simd = D == 128 && PL == 3 && BWD ? 1 : 2;
+    static constexpr bool ahead = !((BWD && (D == 128 || PL == 3)) || (D == 128 && PL == 3));
+};
+
 template <int D, int PL, int ACT, bool BWD>
-__global__ __launch_bounds__(64 * kRowWaves, (PL == 1 ? 2 : 1)) void ffn_rows_kernel(RowsArgs r) {
+__global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) void ffn_rows_kernel(RowsArgs r) {
     using W = Weights<D, PL, BWD>;
+    using Cut = RowsCut<D, PL, BWD>;
     constexpr int S = D / 16, TILES = D / 32;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     extern __shared__ unsigned char lds[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
     const int64_t row = ((int64_t)blockIdx.x * kRowWaves + wave) * 32 + m;
-    const int c0 = 0, c1 = r.a.chunks;
+    const int c1 = r.a.chunks;
     auto first = [&](int c) { return lds + (W::twice ? (c & 1) * (W::first + W::second) * kFrag : 0); };
     auto second = [&](int c) { return first(c) + W::first * kFrag; };
     auto fetch_first = [&](int c) { if (c < c1) fetch<W::first>(r.packed + (size_t)c * (W::first + W::second) * kFrag, first(c)); };
     auto fetch_second = [&](int c) { if (c < c1) fetch<W::second>(r.packed + ((size_t)c * (W::first + W::second) + W::first) * kFrag, second(c)); };
-    fetch_first(c0);
+    fetch_first(0);
     if (W::twice) {
-        fetch_first(c0 + 1);
-        fetch_second(c0);
+        if (Cut::ahead) fetch_first(1);
+        fetch_second(0);
     }
     bf16x8 x[S][PL], dy[BWD ? S : 1][PL];
     v16f y[TILES];
@@ -125,12 +131,34 @@ __global__ __launch_bounds__(64 * kRowWaves, (PL == 1 ? 2 : 1)) void ffn_rows_ke
         mul_add<PL>(o.f[1], x[s], h.u);
         if constexpr (BWD) mul_add<PL>(o.f[2], dy[s], h.dh);
     };
+    auto result = [&](int c, const float (&v)[16], const float (&v2)[16]) {
+        SecondOps o = read_second(second(c), 0);
+        bf16x8 p[2][PL], p2[2][PL];
+        auto round = [&](int s) {
+            planes8<PL>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
+            if constexpr (BWD) planes8<PL>(*reinterpret_cast<const float(*)[8]>(v2 + 8 * s), p2[s]);
+        };
+        round(0);
+#pragma unroll
+        for (int q = 0; q < S; ++q) {
+            SecondOps ahead;
+            if (q + 1 < S) ahead = read_second(second(c), q + 1);
+            fence();
+            const int s = q / TILES, t = q % TILES;
+            mul_add<PL>(o.f[0], p[s], y[t]);
+            if constexpr (BWD) mul_add<PL>(o.f[1], p2[s], y[t]);
+            if (q == 0) round(1);
+            fence();
+            o = ahead;
+        }
+    };
     auto none = [&](Hidden<BWD>& h) {
         clear(h.g);
         clear(h.u);
         if constexpr (BWD) clear(h.dh);
     };
-    auto chunk = [&](auto more, int c, Hidden<BWD>& now, Hidden<BWD>& next) {      // more: there is a chunk c + 1
+    // Chunk c from its hidden values: activations, and its share of the result; between the activations chunk c + 1's products (more).
+    auto chunk = [&](auto more, int c, Hidden<BWD>& now, Hidden<BWD>& next) {
         arrived();
         if (W::twice) {
             fetch_first(c + 2);
@@ -161,48 +189,61 @@ __global__ __launch_bounds__(64 * kRowWaves, (PL == 1 ? 2 : 1)) void ffn_rows_ke
             arrived();
             fetch_first(c + 2);
         }
-        SecondOps o = read_second(second(c), 0);
-        bf16x8 p[2][PL], p2[2][PL];
-        auto round = [&](int s) {
-            planes8<PL>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
-            if constexpr (BWD) planes8<PL>(*reinterpret_cast<const float(*)[8]>(v2 + 8 * s), p2[s]);
-        };
-        round(0);
-#pragma unroll
-        for (int q = 0; q < S; ++q) {
-            SecondOps ahead;
-            if (q + 1 < S) ahead = read_second(second(c), q + 1);
-            fence();
-            const int s = q / TILES, t = q % TILES;
-            mul_add<PL>(o.f[0], p[s], y[t]);
-            if constexpr (BWD) mul_add<PL>(o.f[1], p2[s], y[t]);
-            if (q == 0) round(1);
-            fence();
-            o = ahead;
-        }
+        result(c, v, v2);
     };
     Hidden<BWD> a, b;
-    none(a);
-    arrived();
+    if constexpr (Cut::ahead) {
+        none(a);
+        arrived();
 #pragma unroll
-    for (int s = 0; s < S; ++s) form(read_first(first(c0), s), s, a);
-    if (!W::twice) {
-        __syncthreads();
-        fetch_first(c0 + 1);
-    }
-    // (two at a time: the sets of hidden values change places without being moved)
-    constexpr std::true_type more;
-    constexpr std::false_type last;
-    int c = c0;
-    for (; c + 2 < c1; c += 2) {
-        chunk(more, c, a, b);
-        chunk(more, c + 1, b, a);
-    }
-    if (c + 1 < c1) {
-        chunk(more, c, a, b);
-        chunk(last, c + 1, b, a);
+        for (int s = 0; s < S; ++s) form(read_first(first(0), s), s, a);
+        if (!W::twice) {
+            __syncthreads();
+            fetch_first(1);
+        }
+        // (two at a time: the sets of hidden values change places without being moved)
+        constexpr std::true_type more;
+        constexpr std::false_type last;
+        int c = 0;
+        for (; c + 2 < c1; c += 2) {
+            chunk(more, c, a, b);
+            chunk(more, c + 1, b, a);
+        }
+        if (c + 1 < c1) {
+            chunk(more, c, a, b);
+            chunk(last, c + 1, b, a);
+        } else {
+            chunk(last, c, a, b);
+        }
     } else {
-        chunk(last, c, a, b);
+        for (int c = 0; c < c1; ++c) {
+            arrived();
+            if (W::twice) {
+                fetch_first(c + 1);
+                fetch_second(c + 1);
+            } else {
+                fetch_second(c);
+            }
+            none(a);
+            FirstOps o = read_first(first(c), 0);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                FirstOps ahead;
+                if (s + 1 < S) ahead = read_first(first(c), s + 1);
+                fence();
+                form(o, s, a);
+                fence();
+                o = ahead;
+            }
+            if (!W::twice) {
+                arrived();
+                fetch_first(c + 1);
+            }
+            float v[16], v2[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) activate<ACT>(a, j, v[j], v2[j]);
+            result(c, v, v2);
+        }
     }
     store_result<D, PL>(r, 0, row, kh, y);
 }
