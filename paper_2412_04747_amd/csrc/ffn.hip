@@ -76,6 +76,7 @@ template <int D, int PL, bool BWD> struct Weights {
 template <int D, int PL, bool BWD> struct RowsCut {
     static constexpr int per_simd = D == 128 && PL == 3 && BWD ? 1 : 2;
     static constexpr bool ahead = !((BWD && (D == 128 || PL == 3)) || (D == 128 && PL == 3));
+    static constexpr int depth = PL == 1 ? (BWD ? 3 : 4) : 2;     // steps of the second products that an operand is read ahead, and one
 };
 
 template <int D, int PL, int ACT, bool BWD>
@@ -131,8 +132,9 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) vo
         mul_add<PL>(o.f[1], x[s], h.u);
         if constexpr (BWD) mul_add<PL>(o.f[2], dy[s], h.dh);
     };
-    auto result = [&](int c, const float (&v)[16], const float (&v2)[16]) {
-        SecondOps o = read_second(second(c), 0);
+    // early: the operands of the first steps are on their way already
+    constexpr int DEPTH = Cut::depth < S ? Cut::depth : S;
+    auto result = [&](int c, SecondOps (&o)[DEPTH], const float (&v)[16], const float (&v2)[16]) {
         bf16x8 p[2][PL], p2[2][PL];
         auto round = [&](int s) {
             planes8<PL>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
@@ -141,16 +143,18 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) vo
         round(0);
 #pragma unroll
         for (int q = 0; q < S; ++q) {
-            SecondOps ahead;
-            if (q + 1 < S) ahead = read_second(second(c), q + 1);
+            if (q + DEPTH - 1 < S) o[(q + DEPTH - 1) % DEPTH] = read_second(second(c), q + DEPTH - 1);
             fence();
             const int s = q / TILES, t = q % TILES;
-            mul_add<PL>(o.f[0], p[s], y[t]);
-            if constexpr (BWD) mul_add<PL>(o.f[1], p2[s], y[t]);
+            mul_add<PL>(o[q % DEPTH].f[0], p[s], y[t]);
+            if constexpr (BWD) mul_add<PL>(o[q % DEPTH].f[1], p2[s], y[t]);
             if (q == 0) round(1);
             fence();
-            o = ahead;
         }
+    };
+    auto read_early = [&](int c, SecondOps (&o)[DEPTH]) {
+#pragma unroll
+        for (int q = 0; q < DEPTH - 1; ++q) o[q] = read_second(second(c), q);
     };
     auto none = [&](Hidden<BWD>& h) {
         clear(h.g);
@@ -167,6 +171,7 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) vo
             fetch_second(c);
         }
         float v[16], v2[16];
+        SecondOps early[DEPTH];
         if constexpr (more()) {
             none(next);
             FirstOps o = read_first(first(c + 1), 0);
@@ -174,22 +179,29 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) vo
             for (int s = 0; s < S; ++s) {
                 FirstOps ahead;
                 if (s + 1 < S) ahead = read_first(first(c + 1), s + 1);
+                if (W::twice && s == S - 1) read_early(c, early);
                 fence();
                 form(o, s, next);
 #pragma unroll
-                for (int j = 0; j < 16 / S; ++j) activate<ACT>(now, 16 / S * s + j, v[16 / S * s + j], v2[16 / S * s + j]);
+                for (int j = 16 / S * s; j < 16 / S * (s + 1); ++j) {
+                    activate<ACT>(now, j, v[j], v2[j]);
+                    asm volatile("" : "+v"(v[j]));         // (here, and not together with the others as vectors)
+                    if constexpr (BWD) asm volatile("" : "+v"(v2[j]));
+                }
                 fence();
                 o = ahead;
             }
         } else {
+            if (W::twice) read_early(c, early);
 #pragma unroll
             for (int j = 0; j < 16; ++j) activate<ACT>(now, j, v[j], v2[j]);
         }
         if (!W::twice) {
             arrived();
             fetch_first(c + 2);
+            read_early(c, early);
         }
-        result(c, v, v2);
+        result(c, early, v, v2);
     };
     Hidden<BWD> a, b;
     if constexpr (Cut::ahead) {
@@ -240,9 +252,11 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) vo
                 fetch_first(c + 1);
             }
             float v[16], v2[16];
+            SecondOps early[DEPTH];
+            read_early(c, early);
 #pragma unroll
             for (int j = 0; j < 16; ++j) activate<ACT>(a, j, v[j], v2[j]);
-            result(c, v, v2);
+            result(c, early, v, v2);
         }
     }
     store_result<D, PL>(r, 0, row, kh, y);
