@@ -253,13 +253,24 @@ def rgnn_clip_workspace_bytes(sizes):
     return b.value
 
 
+def addresses(tensors):
+    """The pointer table of a list of torch tensors or raw pointers."""
+    return (_P * len(tensors))(*map(_addr, tensors))
+
+
+def clip_tables(sizes, dtypes):
+    """The size and type tables of rgnn_clip_grad_norm, for a caller that keeps them."""
+    return (C.c_int64 * len(sizes))(*sizes), (C.c_int32 * len(dtypes))(*dtypes)
+
+
 def rgnn_clip_grad_norm(grads, clipped, sizes, dtypes, max_norm, norm, workspace, stream=None):
-    """grads, clipped: lists of torch tensors or raw pointers; clipped may be None (the norm alone)."""
-    n = len(grads)
-    given = (_P * n)(*map(_addr, grads))
-    results = None if clipped is None else given if clipped is grads else (_P * n)(*map(_addr, clipped))
-    _check(lib().rgnn_clip_grad_norm(n, given, results, (C.c_int64 * n)(*sizes), (C.c_int32 * n)(*dtypes), max_norm, _addr(norm),
-                                     _addr(workspace), stream))
+    """grads, clipped: lists of torch tensors or raw pointers, or their `addresses`; clipped may be None (the norm alone).  sizes, dtypes:
+    lists, or what `clip_tables` made of them."""
+    given = grads if isinstance(grads, C.Array) else addresses(grads)
+    results = None if clipped is None else given if clipped is grads else clipped if isinstance(clipped, C.Array) else addresses(clipped)
+    if not isinstance(sizes, C.Array):
+        sizes, dtypes = clip_tables(sizes, dtypes)
+    _check(lib().rgnn_clip_grad_norm(len(given), given, results, sizes, dtypes, max_norm, _addr(norm), _addr(workspace), stream))
 
 
 def rgnn_profile_select(name=None):

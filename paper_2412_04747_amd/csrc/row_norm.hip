@@ -7,7 +7,9 @@
 // Ten operations per element against 8 to 16 bytes: the memory's rate is the bound.  A row stays in the registers of the lanes
 // that loaded it (16 bytes each where the width allows), so each tensor is passed once; the two means of the backward are summed
 // over those lanes together, and q is formed again from s instead of being stored.  Narrow rows share a wavefront: a row of 64
-// fp32 columns is 16 lanes.  Rows wider than a wavefront's 64 vectors, or its registers, are a workgroup's.
+// fp32 columns is 16 lanes.  Rows of more than 256 vectors are a workgroup's.
+// Measured against 4.8 .. 5.3 TB/s of a large copy: 1M rows of 64, fp32 to bf16, forward 181 us (4.9 TB/s); 2M rows of 128, bf16, forward 380 us (5.4),
+// backward 430 (4.8).
 // dw: a workgroup walks its rows with its columns' sums in registers and leaves one partial row; a second launch sums those in order,
 // so results do not depend on timing.
 #include "rgnn_internal.h"
@@ -22,15 +24,38 @@ constexpr int kBlock = 512;              // threads of a workgroup
 constexpr int kMaxBlocks = 1024;         // four per compute unit hold all 32 wavefronts of its SIMDs
 constexpr int kMaxWidth = 8192;
 
-template <typename T, int V>
-__device__ __forceinline__ void load_v(const T* p, float (&v)[V]) {
-    if constexpr (V == 1) v[0] = widen(*p);
-    else load_cols<V>(p, v);
+// Columns c .. c + V - 1 of a row, those before `width`.  EVEN: the width is a multiple of V and rows start at multiples of 16 bytes (8 for
+// four bf16); otherwise the last vector may be short, and vectors lie at any multiple of their element's size, which the
+// hardware loads and stores as well (with single columns / so: 2M rows of 33 fp32 columns, backward, 318 / 205 us; 100000 rows of 257 bf16
+// columns, forward, 123 / 45; 30011 rows of 349 fp32 columns, backward, 44 / 35).
+template <bool EVEN, int V, typename T>
+__device__ __forceinline__ void load_v(const T* row, int c, int width, float (&v)[V]) {
+    if constexpr (EVEN) {
+        load_cols<V>(row + c, v);
+    } else if (c + V <= width) {
+        T t[V];
+        __builtin_memcpy(t, row + c, sizeof(t));
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = widen(t[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = c + e < width ? widen(row[c + e]) : 0.f;
+    }
 }
-template <typename T, int V>
-__device__ __forceinline__ void store_v(T* p, const float (&v)[V]) {
-    if constexpr (V == 1) *p = narrow<T>(v[0]);
-    else store_cols<V>(p, v);
+template <bool EVEN, int V, typename T>
+__device__ __forceinline__ void store_v(T* row, int c, int width, const float (&v)[V]) {
+    if constexpr (EVEN) {
+        store_cols<V>(row + c, v);
+    } else if (c + V <= width) {
+        T t[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) t[e] = narrow<T>(v[e]);
+        __builtin_memcpy(row + c, t, sizeof(t));
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (c + e < width) row[c + e] = narrow<T>(v[e]);
+    }
 }
 
 // Sum over the G lanes of a row (G a power of two up to 64), or over the workgroup.
@@ -79,7 +104,7 @@ struct FwdArgs {
     void* sum; void* out;
 };
 
-template <typename TX, typename TS, typename TO, int V, int NV>
+template <typename TX, typename TS, typename TO, int V, int NV, bool EVEN>
 __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(FwdArgs a) {
     __shared__ float lds[4 * (kBlock / 64)];
     const Shape sh(a.G);
@@ -89,7 +114,7 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(FwdArgs a) {
     for (int j = 0; j < NV; ++j) {
         const int c = (sh.lane + j * sh.G) * V;
         zero_cols<V>(w[j]);
-        if (c < a.width) load_v<float, V>(a.w + c, w[j]);
+        if (c < a.width) load_v<EVEN>(a.w, c, a.width, w[j]);
     }
     int turn = 0;
     // (the trip count is the same for all threads of a workgroup whose rows are its own: the barrier in row_sums)
@@ -103,10 +128,10 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(FwdArgs a) {
             const int c = (sh.lane + j * sh.G) * V;
             zero_cols<V>(s[j]);
             if (live && c < a.width) {
-                load_v<TX, V>(static_cast<const TX*>(a.x) + base + c, s[j]);
+                load_v<EVEN>(static_cast<const TX*>(a.x) + base, c, a.width, s[j]);
                 if (a.r) {
                     float r[V];
-                    load_v<TS, V>(static_cast<const TS*>(a.r) + base + c, r);
+                    load_v<EVEN>(static_cast<const TS*>(a.r) + base, c, a.width, r);
 #pragma unroll
                     for (int e = 0; e < V; ++e) s[j][e] += r[e];
                 }
@@ -119,11 +144,11 @@ __global__ __launch_bounds__(kBlock) void norm_fwd_kernel(FwdArgs a) {
         for (int j = 0; j < NV; ++j) {
             const int c = (sh.lane + j * sh.G) * V;
             if (live && c < a.width) {
-                if (a.sum) store_v<TS, V>(static_cast<TS*>(a.sum) + base + c, s[j]);
+                if (a.sum) store_v<EVEN>(static_cast<TS*>(a.sum) + base, c, a.width, s[j]);
                 float y[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) y[e] = s[j][e] * q * w[j][e];
-                store_v<TO, V>(static_cast<TO*>(a.out) + base + c, y);
+                store_v<EVEN>(static_cast<TO*>(a.out) + base, c, a.width, y);
             }
         }
     }
@@ -138,18 +163,17 @@ struct BwdArgs {
     float* part;             // [gridDim.x][width], or null: dw is not wanted
 };
 
-template <typename T, int V>
-__device__ __forceinline__ void put(void* to, int64_t at, const float (&v)[V], int accumulate) {
-    T* const p = static_cast<T*>(to) + at;
+template <bool EVEN, typename T, int V>
+__device__ __forceinline__ void put(T* row, int c, int width, const float (&v)[V], int accumulate) {
     float t[V];
     zero_cols<V>(t);
-    if (accumulate) load_v<T, V>(p, t);
+    if (accumulate) load_v<EVEN>(row, c, width, t);
 #pragma unroll
     for (int e = 0; e < V; ++e) t[e] += v[e];
-    store_v<T, V>(p, t);
+    store_v<EVEN>(row, c, width, t);
 }
 
-template <typename TX, typename TS, typename TO, int V, int NV>
+template <typename TX, typename TS, typename TO, int V, int NV, bool EVEN>
 __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
     extern __shared__ float lds[];           // row_sums' halves, then a row of sums per wavefront
     const Shape sh(a.G);
@@ -160,7 +184,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
         const int c = (sh.lane + j * sh.G) * V;
         zero_cols<V>(w[j]);
         zero_cols<V>(dw[j]);
-        if (c < a.width) load_v<float, V>(a.w + c, w[j]);
+        if (c < a.width) load_v<EVEN>(a.w, c, a.width, w[j]);
     }
     int turn = 0;
     for (int64_t row0 = (int64_t)blockIdx.x * sh.rows_per_block; row0 < a.rows; row0 += (int64_t)gridDim.x * sh.rows_per_block, ++turn) {
@@ -175,9 +199,9 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
             zero_cols<V>(dy[j]);
             zero_cols<V>(ds[j]);
             if (live && c < a.width) {
-                load_v<TS, V>(static_cast<const TS*>(a.s) + base + c, s[j]);
-                load_v<TO, V>(static_cast<const TO*>(a.dy) + base + c, dy[j]);
-                if (a.ds) load_v<TS, V>(static_cast<const TS*>(a.ds) + base + c, ds[j]);
+                load_v<EVEN>(static_cast<const TS*>(a.s) + base, c, a.width, s[j]);
+                load_v<EVEN>(static_cast<const TO*>(a.dy) + base, c, a.width, dy[j]);
+                if (a.ds) load_v<EVEN>(static_cast<const TS*>(a.ds) + base, c, a.width, ds[j]);
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -197,8 +221,8 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
                     d[e] = ds[j][e] + q * (dy[j][e] * w[j][e] - s[j][e] * along);
                     dw[j][e] += dy[j][e] * (s[j][e] * q);
                 }
-                if (a.dx) put<TX, V>(a.dx, base + c, d, a.accumulate);
-                if (a.dr) put<TS, V>(a.dr, base + c, d, a.accumulate);
+                if (a.dx) put<EVEN>(static_cast<TX*>(a.dx) + base, c, a.width, d, a.accumulate);
+                if (a.dr) put<EVEN>(static_cast<TS*>(a.dr) + base, c, a.width, d, a.accumulate);
             }
         }
     }
@@ -208,7 +232,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (sh.lane + j * sh.G) * V;
-            if (c < a.width) store_v<float, V>(mine + c, dw[j]);
+            if (c < a.width) store_v<EVEN>(mine, c, a.width, dw[j]);
         }
         return;
     }
@@ -221,7 +245,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
         for (int e = 0; e < V; ++e) {
             float v = dw[j][e];
             for (int o = sh.G; o < 64; o <<= 1) v += __shfl_xor(v, o);
-            if ((threadIdx.x & 63) < sh.G && c < a.width) per_wave[(threadIdx.x >> 6) * a.width + c + e] = v;
+            if ((threadIdx.x & 63) < sh.G && c + e < a.width) per_wave[(threadIdx.x >> 6) * a.width + c + e] = v;
         }
     }
     __syncthreads();
@@ -249,13 +273,14 @@ __global__ __launch_bounds__(1024) void norm_dw_kernel(const float* part, int n,
 }
 
 // Columns per vector, lanes per row and vectors per lane.  A vector is 16 bytes of the narrowest type among the tensors, at most 8
-// columns, where the width is a multiple of it; single columns otherwise.
+// columns, where the width is a multiple of it; otherwise four columns.  Up to four vectors per lane a row is a wavefront's, whose lanes sum
+// without a barrier; a wider one is a workgroup's (8192 columns are four vectors of four again, two of eight).
 struct Plan { int V, G, NV, blocks; };
 Plan plan(const rgnn_norm_desc_t* d) {
     const bool all16 = d->x_dtype == RGNN_BF16 && d->sum_dtype == RGNN_BF16 && d->out_dtype == RGNN_BF16;
     Plan p;
-    p.V = all16 && d->width % 8 == 0 ? 8 : d->width % 4 == 0 ? 4 : 1;
-    const int vectors = d->width / p.V;
+    p.V = all16 && d->width % 8 == 0 ? 8 : 4;
+    const int vectors = (d->width + p.V - 1) / p.V;
     p.G = 1;
     while (p.G < vectors && p.G < 64) p.G *= 2;
     if (vectors > 4 * 64) p.G = kBlock;
@@ -265,41 +290,33 @@ Plan plan(const rgnn_norm_desc_t* d) {
     return p;
 }
 
-template <typename TX, typename TS, typename TO, typename F>
-rgnn_status_t with_vectors(const Plan& p, F f) {
-    // (a workgroup's lanes hold 8192 columns in 16 single ones, 4 vectors of four, 2 of eight)
-    if (p.V == 8) {
-        if (p.NV <= 1) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
-        if (p.NV <= 2) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 2>{});
-        return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 4>{});
-    }
-    if (p.V == 4) {
-        if (p.NV <= 1) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
-        if (p.NV <= 2) return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 2>{});
-        return f(std::integral_constant<int, 4>{}, std::integral_constant<int, 4>{});
-    }
-    if (p.NV <= 1) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{});
-    if (p.NV <= 4) return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 4>{});
-    return f(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
+template <int N> using Int = std::integral_constant<int, N>;
+template <typename F>
+rgnn_status_t with_vectors(const rgnn_norm_desc_t* d, const Plan& p, F f) {
+    auto count = [&](auto V, auto even) {
+        return p.NV <= 1 ? f(V, Int<1>{}, even) : p.NV <= 2 ? f(V, Int<2>{}, even) : f(V, Int<4>{}, even);
+    };
+    if (p.V == 8) return count(Int<8>{}, std::true_type{});
+    return d->width % 4 == 0 ? count(Int<4>{}, std::true_type{}) : count(Int<4>{}, std::false_type{});
 }
 
 template <typename TX, typename TS, typename TO>
-rgnn_status_t launch_fwd(const Plan& p, const FwdArgs& a, hipStream_t st) {
-    return with_vectors<TX, TS, TO>(p, [&](auto V, auto NV) -> rgnn_status_t {
+rgnn_status_t launch_fwd(const rgnn_norm_desc_t* d, const Plan& p, const FwdArgs& a, hipStream_t st) {
+    return with_vectors(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
         KernelTimer timer(st, "norm_fwd");
-        norm_fwd_kernel<TX, TS, TO, V(), NV()><<<p.blocks, kBlock, 0, st>>>(a);
+        norm_fwd_kernel<TX, TS, TO, V(), NV(), even()><<<p.blocks, kBlock, 0, st>>>(a);
         RGNN_CHECK_LAUNCH();
         return RGNN_OK;
     });
 }
 template <typename TX, typename TS, typename TO>
-rgnn_status_t launch_bwd(const Plan& p, const BwdArgs& a, hipStream_t st) {
-    return with_vectors<TX, TS, TO>(p, [&](auto V, auto NV) -> rgnn_status_t {
+rgnn_status_t launch_bwd(const rgnn_norm_desc_t* d, const Plan& p, const BwdArgs& a, hipStream_t st) {
+    return with_vectors(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
         // at most 8 wavefronts' rows of 64 x 4 vectors of eight columns: 64 KB
         const size_t lds = sizeof(float) * (4 + (p.G <= 64 && a.part ? a.width : 0)) * (kBlock / 64);
-        RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(norm_bwd_kernel<TX, TS, TO, V(), NV()>), lds));
+        RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(norm_bwd_kernel<TX, TS, TO, V(), NV(), even()>), lds));
         KernelTimer timer(st, "norm_bwd");
-        norm_bwd_kernel<TX, TS, TO, V(), NV()><<<p.blocks, kBlock, lds, st>>>(a);
+        norm_bwd_kernel<TX, TS, TO, V(), NV(), even()><<<p.blocks, kBlock, lds, st>>>(a);
         RGNN_CHECK_LAUNCH();
         return RGNN_OK;
     });
@@ -355,7 +372,7 @@ extern "C" rgnn_status_t rgnn_norm_fwd(const rgnn_norm_desc_t* desc, const void*
     const Plan p = plan(desc);
     const FwdArgs a{desc->rows, desc->width, p.G, desc->eps, x, residual, weight, sum, out};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return with_types(desc, [&](auto tx, auto ts, auto to) { return launch_fwd<decltype(tx), decltype(ts), decltype(to)>(p, a, st); });
+    return with_types(desc, [&](auto tx, auto ts, auto to) { return launch_fwd<decltype(tx), decltype(ts), decltype(to)>(desc, p, a, st); });
 }
 
 extern "C" rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const float* weight, const void* dOut, const void* dSum,
@@ -385,7 +402,7 @@ extern "C" rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void*
         if (dX || dResidual || dWeight) {
             const BwdArgs a{desc->rows, desc->width, p.G, accumulate, desc->eps, sum, weight, dOut, dSum, dX, dResidual,
                             dWeight ? static_cast<float*>(workspace) : nullptr};
-            RGNN_TRY(with_types(desc, [&](auto tx, auto ts, auto to) { return launch_bwd<decltype(tx), decltype(ts), decltype(to)>(p, a, st); }));
+            RGNN_TRY(with_types(desc, [&](auto tx, auto ts, auto to) { return launch_bwd<decltype(tx), decltype(ts), decltype(to)>(desc, p, a, st); }));
         }
     }
     if (dWeight && (desc->rows > 0 || !accumulate)) {

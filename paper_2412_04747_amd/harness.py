@@ -227,14 +227,16 @@ class FfnLayer:
 
 
 class GradClip:
-    """The workspace and result buffers for clipping tensors of the sizes and types of `like`, in place or into `clipped`."""
+    """The workspace, tables and result buffers for clipping tensors of the sizes and types of `like`, in place or into `clipped`."""
 
     def __init__(self, like, in_place=True):
-        self.sizes = [t.numel() for t in like]
-        self.dtypes = [B.RGNN_BF16 if t.dtype == torch.bfloat16 else B.RGNN_F32 for t in like]
-        self.ws = _buf(B.rgnn_clip_workspace_bytes(self.sizes))
+        sizes = [t.numel() for t in like]
+        self.ws = _buf(B.rgnn_clip_workspace_bytes(sizes))
+        self.sizes, self.dtypes = B.clip_tables(sizes, [B.RGNN_BF16 if t.dtype == torch.bfloat16 else B.RGNN_F32 for t in like])
         self.norm = torch.empty((), device="cuda")
         self.clipped = None if in_place else [torch.empty_like(t) for t in like]
+        self._to = None if in_place else B.addresses(self.clipped)
 
     def clip(self, grads, max_norm):
-        B.rgnn_clip_grad_norm(grads, self.clipped or grads, self.sizes, self.dtypes, max_norm, self.norm, self.ws, _stream())
+        given = B.addresses(grads)
+        B.rgnn_clip_grad_norm(given, given if self._to is None else self._to, self.sizes, self.dtypes, max_norm, self.norm, self.ws, _stream())

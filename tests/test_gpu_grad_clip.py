@@ -110,7 +110,7 @@ def test_norm_alone_and_repeatable():
     before = [g.clone() for g in grads]
     alone = torch.zeros((), device="cuda")
     twice = grads + grads[:1]                            # the norm alone may read a tensor twice
-    sizes, types = L.sizes + L.sizes[:1], L.dtypes + L.dtypes[:1]
+    sizes, types = [*L.sizes, L.sizes[0]], [*L.dtypes, L.dtypes[0]]
     ws = torch.empty(B.rgnn_clip_workspace_bytes(sizes), dtype=torch.uint8, device="cuda")
     B.rgnn_clip_grad_norm(grads, None, L.sizes, L.dtypes, float("nan"), alone, ws)
     assert torch.equal(alone, norm) and all(torch.equal(a, b) for a, b in zip(before, grads))
