@@ -37,24 +37,28 @@ constexpr int64_t kIsBf16 = INT64_MIN;
 struct Piece { const void* g; void* out; int64_t beg, end; bool bf16; };
 
 // The workgroup's piece: the last tensor whose first workgroup is not after it.  (Empty tensors have no workgroups.)
-__device__ __forceinline__ Piece find_piece(const Table& t, int64_t piece) {
+__device__ __forceinline__ Piece find_piece(const Table& t, int64_t piece, int block) {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (t.first[mid] <= (int)blockIdx.x) lo = mid;
+        if (t.first[mid] <= block) lo = mid;
         else hi = mid - 1;
     }
-    const int64_t n = t.n[lo] & ~kIsBf16, beg = ((int64_t)blockIdx.x - t.first[lo]) * piece;
+    const int64_t n = t.n[lo] & ~kIsBf16, beg = ((int64_t)block - t.first[lo]) * piece;
     return Piece{t.g[lo], t.out[lo], beg, min(beg + piece, n), t.n[lo] < 0};
 }
 
-// Calls f(pointer to V elements' index) over [beg, end): vectors of V elements where `vec`, single ones for the rest.
+// Calls fv(i, n) with n vectors of V elements at i, i + kThreads V, .. over [beg, end) where `vec` (four at once, so that four loads are on their way),
+// and f1(i) with the single elements left.
 template <int V, typename FV, typename F1>
 __device__ __forceinline__ void for_piece(int64_t beg, int64_t end, bool vec, FV fv, F1 f1) {
     int64_t i = beg;
     if (vec) {
+        constexpr int64_t step = kThreads * V;
         const int64_t whole = beg + (end - beg) / V * V;
-        for (int64_t k = beg + (int64_t)threadIdx.x * V; k < whole; k += kThreads * V) fv(k);
+        int64_t k = beg + (int64_t)threadIdx.x * V;
+        for (; k + 3 * step < whole; k += 4 * step) fv(k, std::integral_constant<int, 4>{});
+        for (; k < whole; k += step) fv(k, std::integral_constant<int, 1>{});
         i = whole;
     }
     for (i += threadIdx.x; i < end; i += kThreads) f1(i);
@@ -76,11 +80,14 @@ template <typename T>
 __device__ __forceinline__ double squares(const T* g, int64_t beg, int64_t end) {
     constexpr int V = RowT<T>::V;
     double s[2] = {0.0, 0.0};
-    for_piece<V>(beg, end, aligned16(g), [&](int64_t i) {
-        float v[V];
-        load_cols<V>(g + i, v);
+    for_piece<V>(beg, end, aligned16(g), [&](int64_t i, auto n) {
+        float v[n()][V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[e & 1] += (double)v[e] * (double)v[e];
+        for (int k = 0; k < n(); ++k) load_cols<V>(g + i + k * kThreads * V, v[k]);
+#pragma unroll
+        for (int k = 0; k < n(); ++k)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[e & 1] += (double)v[k][e] * (double)v[k][e];
     }, [&](int64_t i) {
         const double v = widen(g[i]);
         s[0] += v * v;
@@ -90,7 +97,7 @@ __device__ __forceinline__ double squares(const T* g, int64_t beg, int64_t end) 
 
 __global__ __launch_bounds__(kThreads) void grad_squares_kernel(Table t, int64_t piece, double* sums) {
     __shared__ double lds[kThreads / 64];
-    const Piece p = find_piece(t, piece);
+    const Piece p = find_piece(t, piece, blockIdx.x);
     const double s = block_sum(p.bf16 ? squares(static_cast<const bf16_t*>(p.g), p.beg, p.end)
                                       : squares(static_cast<const float*>(p.g), p.beg, p.end), lds);
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
@@ -99,12 +106,16 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(Table t, int64_t
 template <typename T>
 __device__ __forceinline__ void scale(const T* g, T* out, int64_t beg, int64_t end, float c) {
     constexpr int V = RowT<T>::V;
-    for_piece<V>(beg, end, aligned16(g) && aligned16(out), [&](int64_t i) {
-        float v[V];
-        load_cols<V>(g + i, v);
+    for_piece<V>(beg, end, aligned16(g) && aligned16(out), [&](int64_t i, auto n) {
+        float v[n()][V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] *= c;
-        store_cols<V>(out + i, v);
+        for (int k = 0; k < n(); ++k) load_cols<V>(g + i + k * kThreads * V, v[k]);
+#pragma unroll
+        for (int k = 0; k < n(); ++k) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[k][e] *= c;
+            store_cols<V>(out + i + k * kThreads * V, v[k]);
+        }
     }, [&](int64_t i) { out[i] = narrow<T>(widen(g[i]) * c); });
 }
 
@@ -118,7 +129,8 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table t, int64_t p
     if (t.count == 0) return;
     double c = max_norm / (total + 1e-6);
     if (c > 1.0 || (max_norm == INFINITY && total == total)) c = 1.0;      // (a NaN stays one)
-    const Piece p = find_piece(t, piece);
+    // last pieces first: they are what the caches still hold of the first pass
+    const Piece p = find_piece(t, piece, gridDim.x - 1 - blockIdx.x);
     if (c == 1.0 && p.g == p.out) return;
     if (p.bf16) scale(static_cast<const bf16_t*>(p.g), static_cast<bf16_t*>(p.out), p.beg, p.end, (float)c);
     else scale(static_cast<const float*>(p.g), static_cast<float*>(p.out), p.beg, p.end, (float)c);
