@@ -21,15 +21,17 @@ namespace rgnn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTable = 128;              // tensors per launch: 3.7 KB of the 4 KB a kernel's arguments may have
+constexpr int kTable = 128;              // tensors per launch: 3.7 KB of the 4 KB a kernel's arguments may have;
+constexpr int kSmallTable = 16;          // of a launch of few, which need not carry them
 constexpr int kPieces = 2048;            // about as many pieces in all: eight workgroups per compute unit
 constexpr int64_t kMinPiece = 4096;      // elements
 
+template <int N>
 struct Table {
-    const void* g[kTable];
-    void* out[kTable];
-    int64_t n[kTable];               // elements; bit 63: bf16
-    int32_t first[kTable + 1];       // first workgroup of the tensor
+    const void* g[N];
+    void* out[N];
+    int64_t n[N];                    // elements; bit 63: bf16
+    int32_t first[N + 1];            // first workgroup of the tensor
     int count;
 };
 constexpr int64_t kIsBf16 = INT64_MIN;
@@ -37,7 +39,8 @@ constexpr int64_t kIsBf16 = INT64_MIN;
 struct Piece { const void* g; void* out; int64_t beg, end; bool bf16; };
 
 // The workgroup's piece: the last tensor whose first workgroup is not after it.  (Empty tensors have no workgroups.)
-__device__ __forceinline__ Piece find_piece(const Table& t, int64_t piece, int block) {
+template <int N>
+__device__ __forceinline__ Piece find_piece(const Table<N>& t, int64_t piece, int block) {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -95,7 +98,8 @@ __device__ __forceinline__ double squares(const T* g, int64_t beg, int64_t end) 
     return s[0] + s[1];
 }
 
-__global__ __launch_bounds__(kThreads) void grad_squares_kernel(Table t, int64_t piece, double* sums) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void grad_squares_kernel(Table<N> t, int64_t piece, double* sums) {
     __shared__ double lds[kThreads / 64];
     const Piece p = find_piece(t, piece, blockIdx.x);
     const double s = block_sum(p.bf16 ? squares(static_cast<const bf16_t*>(p.g), p.beg, p.end)
@@ -120,7 +124,8 @@ __device__ __forceinline__ void scale(const T* g, T* out, int64_t beg, int64_t e
 }
 
 // Workgroup 0 stores the norm (null in the launches after the first).  t.count == 0: the norm alone.
-__global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table t, int64_t piece, const double* sums, int num_sums, float max_norm, float* norm) {
+template <int N>
+__global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table<N> t, int64_t piece, const double* sums, int num_sums, float max_norm, float* norm) {
     __shared__ double lds[kThreads / 64];
     double s = 0.0;
     for (int i = threadIdx.x; i < num_sums; i += kThreads) s += sums[i];
@@ -218,7 +223,7 @@ extern "C" rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* g
     double* const sums = static_cast<double*>(workspace);
     // launches of up to kTable tensors that have elements; `f` gets the table and its number of workgroups
     auto tables = [&](auto f) -> rgnn_status_t {
-        Table t;
+        Table<kTable> t;
         t.count = 0;
         t.first[0] = 0;
         for (int64_t i = 0; i < count; ++i) {
@@ -237,25 +242,36 @@ extern "C" rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* g
         return RGNN_OK;
     };
     int64_t at = 0;
-    RGNN_TRY(tables([&](const Table& t, int blocks) -> rgnn_status_t {
+    auto fitting = [](const Table<kTable>& t, auto f) {
+        if (t.count > kSmallTable) return f(t);
+        Table<kSmallTable> s;
+        s.count = t.count;
+        std::copy(t.g, t.g + t.count, s.g);
+        std::copy(t.out, t.out + t.count, s.out);
+        std::copy(t.n, t.n + t.count, s.n);
+        std::copy(t.first, t.first + t.count + 1, s.first);
+        return f(s);
+    };
+    RGNN_TRY(tables([&](const Table<kTable>& t, int blocks) -> rgnn_status_t {
         KernelTimer timer(st, "grad_squares");
-        grad_squares_kernel<<<blocks, kThreads, 0, st>>>(t, p.piece, sums + at);
+        fitting(t, [&](const auto& u) { grad_squares_kernel<<<blocks, kThreads, 0, st>>>(u, p.piece, sums + at); });
         RGNN_CHECK_LAUNCH();
         at += blocks;
         return RGNN_OK;
     }));
     bool stored = false;
-    auto scale_launch = [&](const Table& t, int blocks) -> rgnn_status_t {
+    auto scale_launch = [&](const Table<kTable>& t, int blocks) -> rgnn_status_t {
         KernelTimer timer(st, "grad_scale");
-        grad_scale_kernel<<<blocks, kThreads, 0, st>>>(t, p.piece, sums, (int)p.pieces, max_norm, stored ? nullptr : norm);
+        fitting(t, [&](const auto& u) { grad_scale_kernel<<<blocks, kThreads, 0, st>>>(u, p.piece, sums, (int)p.pieces, max_norm, stored ? nullptr : norm); });
         RGNN_CHECK_LAUNCH();
         stored = true;
         return RGNN_OK;
     };
     if (clipped) RGNN_TRY(tables(scale_launch));
     if (!stored) {
-        Table none;
+        Table<kTable> none;
         none.count = 0;
+        none.first[0] = 0;
         RGNN_TRY(scale_launch(none, 1));
     }
     return RGNN_OK;
