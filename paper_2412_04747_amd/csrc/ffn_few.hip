@@ -20,7 +20,7 @@ template <int D, int PL, bool BWD> constexpr int rows_lds() { return (BWD ? 5 : 
 
 // 128 rows, a share of the chunks.
 template <int D, int PL, int ACT, bool BWD>
-__device__ __forceinline__ void rows_block(const RowsArgs& r, int block, int split, unsigned char* lds) {
+__device__ __forceinline__ void few_rows_block(const RowsArgs& r, int block, int split, unsigned char* lds) {
     constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
@@ -107,7 +107,7 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int block, int spl
 template <int D, int PL, int ACT>
 __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_fwd_kernel(RowsArgs r) {
     extern __shared__ unsigned char lds[];
-    rows_block<D, PL, ACT, false>(r, blockIdx.x, blockIdx.y, lds);
+    few_rows_block<D, PL, ACT, false>(r, blockIdx.x, blockIdx.y, lds);
 }
 
 // Workgroups [0, row_blocks * r.splits) form dX, the others the weights' gradients.
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_bwd_kernel(RowsArgs
     extern __shared__ unsigned char lds[];
     const int b = blockIdx.x, n = row_blocks * r.splits;
     if (b < n) {
-        rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
+        few_rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
     } else if (k.splits == 1) {
         grad_block<D, PL, ACT, kRowWaves, true>(k, 0, b - n, lds);
     } else {
@@ -140,8 +140,7 @@ int row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 
 int row_splits(const rgnn_ffn_desc_t* d) {
     return chunks_of(d) <= 3 ? 1 : std::max(1, std::min(chunks_of(d), 256 / std::max(row_blocks(d), 1)));
 }
-int grad_group(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }
-int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + grad_group(d) - 1) / grad_group(d); }
+int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + ffn_grad_columns(d) - 1) / ffn_grad_columns(d); }
 // Units of 32 rows: one or two need no division.
 int grad_splits(const rgnn_ffn_desc_t* d) {
     const int units = (int)((d->rows + UNIT - 1) / UNIT);

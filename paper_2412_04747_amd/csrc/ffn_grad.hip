@@ -49,6 +49,15 @@ int ffn_grad_splits(const rgnn_ffn_desc_t* d) {
     return (int)std::min<int64_t>(std::max(8, sizes(d).resident / groups_of(d) / 8 * 8), units);
 }
 
+rgnn_status_t ffn_grad_reduce(const rgnn_ffn_desc_t* d, const FfnGradArgs& k, hipStream_t st) {
+    const unsigned blocks = (unsigned)((int64_t)3 * d->width * k.a.chunks * kHid / 64);
+    KernelTimer timer(st, "ffn_bwd_weights.reduce");
+    if (d->dtype == RGNN_BF16) ffn_grad_reduce_kernel<bf16_t><<<blocks, 256, 0, st>>>(k, d->width);
+    else ffn_grad_reduce_kernel<float><<<blocks, 256, 0, st>>>(k, d->width);
+    RGNN_CHECK_LAUNCH();
+    return RGNN_OK;
+}
+
 rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, void* dWg, void* dWu, void* dWd, hipStream_t st) {
     const FfnGradArgs k{a, part, ffn_grad_splits(d), groups_of(d), dWg, dWu, dWd, (d->flags & RGNN_FLAG_ACCUMULATE) != 0};
     if (k.splits > 0) {
@@ -65,12 +74,7 @@ rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, 
         };
         RGNN_TRY(run());
     }
-    const unsigned blocks = (unsigned)((int64_t)3 * d->width * a.chunks * kHid / 64);
-    KernelTimer timer(st, "ffn_bwd_weights.reduce");
-    if (d->dtype == RGNN_BF16) ffn_grad_reduce_kernel<bf16_t><<<blocks, 256, 0, st>>>(k, d->width);
-    else ffn_grad_reduce_kernel<float><<<blocks, 256, 0, st>>>(k, d->width);
-    RGNN_CHECK_LAUNCH();
-    return RGNN_OK;
+    return ffn_grad_reduce(d, k, st);
 }
 
 }  // namespace rgnn
