@@ -359,7 +359,7 @@ rgnn_status_t rgnn_hgt_bwd(const rgnn_graph_t* g, const rgnn_layer_desc_t* desc,
  * fp32.  The mean of the squares has to be in the range of fp32.
  *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: dX, dResidual and dWeight are added to) */
 typedef struct {
-    int64_t rows;
+    int64_t rows;                /* below 2^31 */
     int32_t width;               /* 1 .. 8192 */
     int32_t x_dtype, sum_dtype, out_dtype;
     float eps;                   /* finite, >= 0 */
@@ -384,11 +384,11 @@ rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const
  *   activation RGNN_ACT_SILU (g / (1 + exp(-g))) or RGNN_ACT_RELU (its derivative at 0 is 0)
  *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: every gradient is added to)
  * RGNN_F32: products are formed from three bfloat16 planes per operand on the matrix cores, as close to 64 bits as fp32
- * products are; operands below 2^-110 lose their last bits.  RGNN_BF16: act(g) u and the gradients of g and u are rounded
+ * products are; operands below 2^-110 lose their last bits, and those above 3.38e38 count as infinite.  RGNN_BF16: act(g) u and the gradients of g and u are rounded
  * to bfloat16 where they enter the next product.  An infinite or NaN entry, or a product that leaves the range of fp32, makes its row
  * of out (dX), and the weights' gradients, NaN or infinite; the other rows are not touched by it. */
 typedef struct {
-    int64_t rows;
+    int64_t rows;                /* up to 2000000000 */
     int32_t dtype;
     int32_t width;               /* 32, 64 or 128 */
     int32_t hidden;              /* 1 .. 16384 */

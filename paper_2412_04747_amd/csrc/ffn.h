@@ -216,12 +216,8 @@ __device__ __forceinline__ void combine_block(const float* part, int splits, int
     store_cols<4>(out + i, sum);
 }
 
-// ffn_grad.hip
-int ffn_grad_splits(const rgnn_ffn_desc_t* d);
-inline int ffn_grad_columns(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }   // of a workgroup of kRowWaves
-struct FfnGradArgs;
-rgnn_status_t ffn_grad_reduce(const rgnn_ffn_desc_t* d, const FfnGradArgs& k, hipStream_t st);
-rgnn_status_t ffn_grad(const rgnn_ffn_desc_t* d, const FfnArgs& a, float* part, void* dWg, void* dWu, void* dWd, hipStream_t st);
+// hidden values of a workgroup that forms the weights' gradients
+inline int ffn_grad_columns(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }
 
 // ffn_few.hip: the same for few rows
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward);

@@ -46,50 +46,40 @@ __global__ __launch_bounds__(256) void ffn_pack_kernel(PackArgs p) {
     for (int k = 0; k < PL; ++k) *reinterpret_cast<bf16x8*>(to + k * kFrag) = f[k];
 }
 
-template <int D, int PL, int ACT, bool BWD>
-__global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, BWD>::per_simd)) void ffn_rows_kernel(RowsArgs r) {
+template <int D, int PL, int ACT>
+__global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, false>::per_simd)) void ffn_fwd_kernel(RowsArgs r) {
     extern __shared__ unsigned char lds[];
-    rows_block<D, PL, ACT, BWD>(r, blockIdx.x, lds);
+    rows_block<D, PL, ACT, false>(r, blockIdx.x, lds);
 }
 
 // The backward's two passes in one launch: workgroups [0, row_blocks) take the rows, the others the weights' gradients.  Neither waits for
 // the other's last workgroups (two launches / one: 16500 rows, d 64, f 256, bf16, 40.8 / 31.9 us; 64000 rows 51.0 / 47.5; 500000 rows, fp32, 921 / 908).
 template <int D, int PL, int ACT>
-__global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, true>::per_simd)) void ffn_both_kernel(RowsArgs r, FfnGradArgs k, int row_blocks) {
+__global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, true>::per_simd)) void ffn_bwd_kernel(RowsArgs r, FfnGradArgs k, int row_blocks) {
     extern __shared__ unsigned char lds[];
     const int b = (int)blockIdx.x - row_blocks;
     if (b < 0) rows_block<D, PL, ACT, true>(r, blockIdx.x, lds);
-    else grad_block<D, PL, ACT, kRowWaves, false>(k, b % k.splits, b / k.splits, lds);
+    else grad_block<D, PL, ACT, false>(k, b % k.splits, b / k.splits, lds);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void ffn_grad_reduce_kernel(FfnGradArgs k, int D) {
+    __shared__ float lds[16][64];
+    grad_reduce_block<T>(k, D, blockIdx.x, lds);
 }
 
 int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
 constexpr int kBlockRows = 32 * kRowWaves;
+constexpr int64_t kMostRows = 2000000000;      // HIP counts a launch's lanes, two per row, in 32 bits
 size_t packed_bytes(const rgnn_ffn_desc_t* d, bool backward) {
     return align_up((size_t)chunks_of(d) * (backward ? 5 : 3) * (d->width / 16) * (d->dtype == RGNN_BF16 ? 1 : 3) * kFrag);
 }
-size_t grad_part_bytes(const rgnn_ffn_desc_t* d, int splits) {
-    return align_up(sizeof(float) * (size_t)splits * 3 * d->width * chunks_of(d) * kHid);
-}
-size_t grad_bytes(const rgnn_ffn_desc_t* d) { return grad_part_bytes(d, ffn_grad_splits(d)); }
-
-// Both passes of the backward in one launch.
-int both_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + ffn_grad_columns(d) - 1) / ffn_grad_columns(d); }
-int both_splits(const rgnn_ffn_desc_t* d) { return (int)std::min<int64_t>(std::max(4, 512 / both_groups(d)), (d->rows + UNIT - 1) / UNIT); }
+// Shares of the rows for the weights' gradients: two workgroups per compute unit with those of all hidden values; no more than units.
+int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + ffn_grad_columns(d) - 1) / ffn_grad_columns(d); }
+int grad_splits(const rgnn_ffn_desc_t* d) { return (int)std::min<int64_t>(std::max(4, 512 / grad_groups(d)), (d->rows + UNIT - 1) / UNIT); }
 size_t workspace_bytes(const rgnn_ffn_desc_t* d, bool backward) {
     if (ffn_few(d, backward)) return ffn_few_bytes(d, backward);
-    if (!backward) return packed_bytes(d, false);
-    return std::max(grad_bytes(d), packed_bytes(d, true) + grad_part_bytes(d, both_splits(d)));
-}
-
-template <int D, int PL, int ACT, bool BWD>
-rgnn_status_t launch_rows(const RowsArgs& r, hipStream_t st) {
-    constexpr size_t lds = Weights<D, PL, BWD>::lds;
-    auto* const kernel = ffn_rows_kernel<D, PL, ACT, BWD>;
-    RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
-    KernelTimer timer(st, BWD ? "ffn_bwd_rows" : "ffn_fwd");
-    kernel<<<(unsigned)((r.a.rows + kBlockRows - 1) / kBlockRows), 64 * kRowWaves, lds, st>>>(r);
-    RGNN_CHECK_LAUNCH();
-    return RGNN_OK;
+    return packed_bytes(d, backward) + (backward ? align_up(sizeof(float) * (size_t)grad_splits(d) * 3 * d->width * chunks_of(d) * kHid) : 0);
 }
 
 template <int D, int PL>
@@ -101,43 +91,58 @@ rgnn_status_t launch_pack(const FfnArgs& a, bool backward, unsigned char* to, hi
     return RGNN_OK;
 }
 
-rgnn_status_t both_passes(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, int accumulate, void* workspace, hipStream_t st) {
+int row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 1) / kBlockRows); }
+
+rgnn_status_t forward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st) {
+    unsigned char* const packed = static_cast<unsigned char*>(workspace);
+    const RowsArgs r{a, packed, out, nullptr, 1, 0};
+    RGNN_DISPATCH_FFN(d, {
+        RGNN_TRY((launch_pack<D, PL>(a, false, packed, st)));
+        constexpr size_t lds = Weights<D, PL, false>::lds;
+        auto* const kernel = ffn_fwd_kernel<D, PL, ACT>;
+        RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
+        KernelTimer timer(st, "ffn_fwd");
+        kernel<<<row_blocks(d), 64 * kRowWaves, lds, st>>>(r);
+        RGNN_CHECK_LAUNCH();
+        return RGNN_OK;
+    });
+}
+
+rgnn_status_t grad_reduce(const rgnn_ffn_desc_t* d, const FfnGradArgs& k, hipStream_t st) {
+    const unsigned blocks = (unsigned)((int64_t)3 * d->width * k.a.chunks * kHid / 64);
+    KernelTimer timer(st, "ffn_bwd.reduce");
+    if (d->dtype == RGNN_BF16) ffn_grad_reduce_kernel<bf16_t><<<blocks, 256, 0, st>>>(k, d->width);
+    else ffn_grad_reduce_kernel<float><<<blocks, 256, 0, st>>>(k, d->width);
+    RGNN_CHECK_LAUNCH();
+    return RGNN_OK;
+}
+
+// dX or the weights' gradients may be null; the other's are the same either way.
+rgnn_status_t backward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, int accumulate, void* workspace, hipStream_t st) {
     unsigned char* const packed = static_cast<unsigned char*>(workspace);
     const RowsArgs r{a, packed, dX, nullptr, 1, accumulate};
-    const FfnGradArgs k{a, reinterpret_cast<float*>(packed + packed_bytes(d, true)), both_splits(d), both_groups(d), dWg, dWu, dWd, accumulate};
+    const FfnGradArgs k{a, reinterpret_cast<float*>(packed + packed_bytes(d, true)), grad_splits(d), grad_groups(d), dWg, dWu, dWd, accumulate};
+    const int rows = dX ? row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
-            RGNN_TRY((launch_pack<D, PL>(a, true, packed, st)));
+            if (rows) RGNN_TRY((launch_pack<D, PL>(a, true, packed, st)));
             constexpr size_t lds = std::max(Weights<D, PL, true>::lds, (size_t)Cut<D, PL>::lds);
-            auto* const kernel = ffn_both_kernel<D, PL, ACT>;
+            auto* const kernel = ffn_bwd_kernel<D, PL, ACT>;
             RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
-            const int blocks = (int)((d->rows + kBlockRows - 1) / kBlockRows);
-            KernelTimer timer(st, "ffn_bwd_both");
-            kernel<<<blocks + k.splits * k.groups, 64 * kRowWaves, lds, st>>>(r, k, blocks);
+            KernelTimer timer(st, "ffn_bwd");
+            kernel<<<rows + grads, 64 * kRowWaves, lds, st>>>(r, k, rows);
             RGNN_CHECK_LAUNCH();
             return RGNN_OK;
         });
     };
-    RGNN_TRY(run());
-    return ffn_grad_reduce(d, k, st);
-}
-
-template <bool BWD>
-rgnn_status_t rows_pass(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, int accumulate, void* workspace, hipStream_t st) {
-    unsigned char* const packed = static_cast<unsigned char*>(workspace);
-    const RowsArgs r{a, packed, out, nullptr, 1, accumulate};
-    auto run = [&]() -> rgnn_status_t {
-        RGNN_DISPATCH_FFN(d, {
-            RGNN_TRY((launch_pack<D, PL>(a, BWD, packed, st)));
-            return launch_rows<D, PL, ACT, BWD>(r, st);
-        });
-    };
-    return run();
+    if (rows + grads) RGNN_TRY(run());
+    return dWg ? grad_reduce(d, k, st) : RGNN_OK;
 }
 
 rgnn_status_t check_desc(const rgnn_ffn_desc_t* d) {
     if (!d) RGNN_FAIL(RGNN_EINVAL, "desc is NULL");
     RGNN_TRY(check_rows(d->rows));
+    if (d->rows > kMostRows) RGNN_FAIL(RGNN_EUNSUPPORTED, "rows %lld not supported (up to %lld)", (long long)d->rows, (long long)kMostRows);
     RGNN_TRY(check_dtype(d->dtype));
     
     if (d->width != 32 && d->width != 64 && d->width != 128) RGNN_FAIL(RGNN_EUNSUPPORTED, "width %d not supported (32/64/128)", d->width);
@@ -186,7 +191,7 @@ extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X
                            {span(out, n, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, false)}}));
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, nullptr};
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    return ffn_few(desc, false) ? ffn_few_fwd(desc, a, out, workspace, st) : rows_pass<false>(desc, a, out, 0, workspace, st);
+    return ffn_few(desc, false) ? ffn_few_fwd(desc, a, out, workspace, st) : forward(desc, a, out, workspace, st);
 }
 
 extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
@@ -205,8 +210,7 @@ extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X
     const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, dOut};
     const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
     if (desc->rows > 0 && ffn_few(desc, true)) return ffn_few_bwd(desc, a, dX, dWg, dWu, dWd, workspace, st);
-    if (dX && grads && desc->rows > 0) return both_passes(desc, a, dX, dWg, dWu, dWd, accumulate, workspace, st);
-    if (dX && desc->rows > 0) RGNN_TRY(rows_pass<true>(desc, a, dX, accumulate, workspace, st));
-    if (grads && (desc->rows > 0 || !accumulate)) RGNN_TRY(ffn_grad(desc, a, static_cast<float*>(workspace), dWg, dWu, dWd, st));
-    return RGNN_OK;
+    if (desc->rows == 0) dX = nullptr;
+    if (!grads || (desc->rows == 0 && accumulate)) dWg = nullptr;
+    return backward(desc, a, dX, dWg, dWu, dWd, accumulate, workspace, st);
 }

@@ -2,7 +2,8 @@
 //
 // The weights are read as they are given and put into the LDS as operands by the workgroups that use them, so that no launch lays them out first;
 // the backward's two passes share a launch, some of its workgroups forming dX and the others the weights' gradients; and what several
-// workgroups add up is summed by one launch for both.  A call is two launches, or one where nothing is divided, against three (forward) and five.
+// workgroups add up is summed by one launch for both.  A call is two launches, or one where nothing is divided.  One row, d 128, f 512, fp32, forward:
+// 11.2 us with the time the caller takes for its call, 15.4 with a launch that lays out the weights; 1000 rows, d 64, f 256, bf16, backward: 13.9 and 32.
 // Every 128 rows read and split all weights again, which is worth it up to some number of rows (ffn_few).
 #include <math.h>
 
@@ -118,9 +119,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_bwd_kernel(RowsArgs
     if (b < n) {
         few_rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
     } else if (k.splits == 1) {
-        grad_block<D, PL, ACT, kRowWaves, true>(k, 0, b - n, lds);
+        grad_block<D, PL, ACT, true>(k, 0, b - n, lds);
     } else {
-        grad_block<D, PL, ACT, kRowWaves, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
+        grad_block<D, PL, ACT, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
     }
 }
 
@@ -168,17 +169,17 @@ rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs
 
 }  // namespace
 
-// Up to which number of rows this is faster than laying out the weights first and taking every pass by itself, in us here / there:
-//   forward   d 32, f 64, bf16: 32000 rows 4.9 / 5.7, 48000 5.5 / 6.3; fp32: 32000 7.8 / 9.3, 48000 11.0 / 11.3
-//             d 64, f 256, bf16: 2000 8.4 / 9.5, 4000 10.4 / 9.6; fp32: 16000 21.9 / 22.4, 24000 25.7 / 22.8
-//             d 128, f 341, bf16: 2000 14.0 / 14.6, 4000 17.8 / 14.7; fp32: 16000 43.9 / 46.5, 24000 56.8 / 47.8
-//   backward  d 32, f 64, bf16: 32000 15.3 / 22.8; fp32: 32000 19.7 / 26.7
-//             d 64, f 256, bf16: 12000 36.2 / 41.6, 24000 50.3 / 42.1; fp32: 16000 57.9 / 61.8, 24000 84.9 / 67.9
-//             d 128, f 341, bf16: 8000 42.4 / 54.3, 12000 57.1 / 55.5; fp32: 16000 138 / 152, 24000 207 / 181
+// Up to which number of rows this is faster than laying out the weights first, in us here / there:
+//   forward   d 32, f 64, bf16: 32000 rows 4.9 / 5.7; fp32: 32000 7.8 / 8.9
+//             d 64, f 256, bf16: 2000 8.3 / 9.4, 4000 10.5 / 9.4; fp32: 12000 19.9 / 20.7, 16000 21.8 / 20.8
+//             d 128, f 341, bf16: 2000 14.3 / 14.2, 4000 18.0 / 14.4; fp32: 12000 41.4 / 44.1, 24000 57.0 / 46.1
+//   backward  d 32, f 64, bf16: 32000 15.4 / 19.9; fp32: 32000 20.1 / 26.1
+//             d 64, f 256, bf16: 3000 24.0 / 24.2, 4000 29.7 / 26.9; fp32: 8000 38.8 / 45.1, 12000 51.9 / 45.3
+//             d 128, f 341, bf16: 4000 35.0 / 35.7, 6000 39.7 / 37.0; fp32: 8000 81.5 / 89.0, 12000 120 / 110
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
     if (d->width == 32) return d->rows <= 32768;
-    if (d->dtype == RGNN_F32) return d->rows <= 16384;
-    return d->rows <= (backward ? 12288 : 2560);
+    if (d->dtype == RGNN_F32) return d->rows <= (backward ? 8192 : 12288);
+    return d->rows <= (backward ? 3584 : 2304);
 }
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d) + (backward ? grad_bytes(d) : 0)); }
 

@@ -1,4 +1,15 @@
-// The gradients of the feed-forward block's weights: a workgroup's work (ffn_grad.hip says how it is laid out).  Internal.
+// The gradients of the feed-forward block's weights: a workgroup's work.  Internal.
+//
+// A wavefront owns MT hidden values: their columns of Wg and Wu and rows of Wd stay in its registers, and so do its columns of the
+// three gradients while it walks the rows, 32 at a time.  Of each unit it forms g, u and dh = dOut Wd^T with the rows along the
+// accumulator's values, which makes act(g) u, dg and du the second operand of X^T dg, X^T du and dOut^T h as they lie; the first
+// is read from the rows' planes in the LDS by the transposing read.  The rows are loaded, split into planes and put there by all
+// wavefronts of the workgroup, one unit ahead.
+// g, u and dh are formed a second time (the pass of the rows has them with the hidden values along): three products more of eleven, against
+// three tensors of the hidden width written and read, six times the bytes of the row tensors at f = 2 d.
+// MT = 32 for bf16 up to width 64; 16 otherwise, so that two wavefronts share a SIMD (fp32, 1M rows, d 64, f 256, this pass alone: 1086 us with 32, 889
+// with 16; bf16, 200017 rows, d 128, f 341: over 600 and 152), or, for fp32 at width 128, that the registers suffice at all.
+// Rows are divided among workgroups in interleaved shares, which another launch adds in order.
 #pragma once
 #include "ffn.h"
 
@@ -6,12 +17,8 @@ namespace rgnn {
 
 constexpr int UNIT = 32;
 
-// Hidden values of a wavefront (MT), wavefronts of a workgroup, and wavefronts that share a SIMD.
 template <int D, int PL> struct Cut {
-    static constexpr bool wide = D == 128 && PL == 3;
-    static constexpr int MT = PL == 1 && D < 128 ? 32 : 16;
-    static constexpr int waves = MT == 32 || wide ? 4 : 8;
-    static constexpr int per_simd = wide ? 1 : 2;
+    static constexpr int MT = PL == 1 && D < 128 ? 32 : 16;      // hidden values of a wavefront
     static constexpr int lds = 2 * 2 * PL * UNIT * D * 2;        // two units of either tensor
 };
 struct FfnGradArgs {
@@ -30,9 +37,9 @@ __device__ __forceinline__ int swizzle(int r) {
 }
 
 // The workgroup's share of the rows, `split`, and of the hidden values, `group`.
-template <int D, int PL, int ACT, int WAVES, bool DIRECT>
+template <int D, int PL, int ACT, bool DIRECT>
 __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int group, unsigned char* lds) {
-    constexpr int MT = Cut<D, PL>::MT;
+    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     using Acc = typename std::conditional<MT == 32, v16f, v4f>::type;
     constexpr int KS = MT == 32 ? 16 : 32;               // contraction of an instruction

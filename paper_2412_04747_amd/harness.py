@@ -238,5 +238,8 @@ class GradClip:
         self._to = None if in_place else B.addresses(self.clipped)
 
     def clip(self, grads, max_norm):
+        """`grads`: tensors of the sizes and types of `like`, in its order."""
+        if len(grads) != len(self.sizes):
+            raise ValueError(f"GradClip.clip: {len(grads)} tensors, made for {len(self.sizes)}")
         given = B.addresses(grads)
         B.rgnn_clip_grad_norm(given, given if self._to is None else self._to, self.sizes, self.dtypes, max_norm, self.norm, self.ws, _stream())

@@ -190,23 +190,39 @@ def test_repeatable_bounded_and_alone(dtype):
             assert not L.out[rows // 2].isfinite().any() and not L.out[0].isfinite().any()
 
 
-def test_accumulate_and_optional_results():
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [33, 3000, 20003])
+def test_accumulate_and_optional_results(rows, dtype):
+    """Gradients added to what is there; a result that is not asked for leaves the others' bits."""
     import torch
     from paper_2412_04747_amd import binding as B
-    for rows in (33, 5000):
-        p = _inputs(rows, 64, 80, "f32", "silu", 41)
-        L, M = _layer(p, "silu"), _layer(p, "silu", B.RGNN_FLAG_ACCUMULATE)
-        L.bwd()
-        for t in M.grads().values():
-            t.fill_(1.0)
-        M.bwd()
-        for k, v in L.grads().items():
-            # the sum rounds once more: half a step at the larger of both
-            assert ((M.grads()[k] - 1.0) - v).abs().max() <= (1 + v.abs().max()) * 2 * U, k
-        dX, dWg = L.dX.clone(), L.dWg.clone()
-        B.rgnn_ffn_bwd(L.desc, L.X, L.Wg, L.Wu, L.Wd, L.dOut, None, L.dWg.zero_(), L.dWu, L.dWd, L.ws)
-        B.rgnn_ffn_bwd(L.desc, L.X, L.Wg, L.Wu, L.Wd, L.dOut, L.dX.zero_(), None, None, None, L.ws)
-        assert torch.equal(L.dX, dX) and torch.equal(L.dWg, dWg)
+    print(f"ffn case rows={rows} {dtype}", flush=True)
+    p = _inputs(rows, 64, 80, dtype, "silu", 41)
+    L, M = _layer(p, "silu"), _layer(p, "silu", B.RGNN_FLAG_ACCUMULATE)
+    L.bwd()
+    for t in M.grads().values():
+        t.fill_(1.0)
+    M.bwd()
+    step = 2.0 ** -8 if dtype == "bf16" else U
+    for k, v in L.grads().items():
+        # a = round(v + 1), b = round(v): half a step of either; fp32 may add in another order, one more
+        v = v.double()
+        assert ((M.grads()[k].double() - 1.0 - v).abs() <= 3.1 * step * (1 + v.abs())).all(), k
+    want = {k: v.clone() for k, v in L.grads().items()}
+    for t in L.grads().values():
+        t.zero_()
+    B.rgnn_ffn_bwd(L.desc, L.X, L.Wg, L.Wu, L.Wd, L.dOut, None, L.dWg, L.dWu, L.dWd, L.ws)
+    assert (L.dX == 0).all() and all(torch.equal(v, want[k]) for k, v in L.grads().items() if k != "dX")
+    for t in L.grads().values():
+        t.zero_()
+    B.rgnn_ffn_bwd(L.desc, L.X, L.Wg, L.Wu, L.Wd, L.dOut, L.dX, None, None, None, L.ws)
+    assert torch.equal(L.dX, want["dX"]) and (L.dWg == 0).all() and (L.dWd == 0).all()
+    B.rgnn_ffn_bwd(L.desc, L.X, L.Wg, L.Wu, L.Wd, L.dOut, None, None, None, None, L.ws)
+
+
+def test_no_rows():
+    from paper_2412_04747_amd import binding as B
+    import torch
     from paper_2412_04747_amd.harness import FfnLayer
     N = FfnLayer(0, 64, 20)
     N.X = N.dOut = torch.empty(0, 64, device="cuda")
@@ -214,6 +230,31 @@ def test_accumulate_and_optional_results():
     N.dWg.fill_(2.0)
     N.fwd(); N.bwd()
     assert (N.dWg == 0).all() and (N.dWu == 0).all() and (N.dWd == 0).all()
+    N.desc.flags = B.RGNN_FLAG_ACCUMULATE
+    N.dWu.fill_(2.0)
+    N.bwd()
+    assert (N.dWu == 2).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_widest_hidden(dtype):
+    """512 chunks, few rows and many."""
+    import torch
+    for rows in (40, 33000):
+        print(f"ffn case rows={rows} width=32 hidden=16384 {dtype}", flush=True)
+        p = _inputs(40, 32, 16384, dtype, "silu", 61)
+        n = (rows + 39) // 40
+        p["X"], p["dOut"] = p["X"].repeat(n, 1)[:rows], torch.cat([p["dOut"], torch.zeros(40 * (n - 1), 32).to(p["dOut"].dtype)])[:rows]
+        L = _layer(p, "silu")
+        L.fwd(); L.bwd()
+        torch.cuda.synchronize()
+        # rows 40 and on repeat the first forty, with a gradient of zeros
+        want = expected({k: v[:40] if k in ("X", "dOut") else v for k, v in p.items()}, "silu", dtype)
+        _check(L.out[:40], want["out"], "out")
+        assert torch.equal(L.out, L.out[:40].repeat(n, 1)[:rows])
+        for k, v in L.grads().items():
+            _check(v[:40] if k == "dX" else v, want[k], k)
+        assert (L.dX[40:] == 0).all()
 
 
 def test_extreme_gates():
