@@ -160,7 +160,7 @@ struct BwdArgs {
     float eps;
     const void* s; const float* w; const void* dy; const void* ds;
     void* dx; void* dr;
-    float* part;             // [gridDim.x][width], or null: dw is not wanted
+    float* part;             // [gridDim.x][width] or, of a single workgroup, dw itself; null: dw is not wanted
 };
 
 template <bool EVEN, typename T, int V>
@@ -228,11 +228,12 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
     }
     if (!a.part) return;
     float* const mine = a.part + (int64_t)blockIdx.x * a.width;
+    const int add = a.accumulate && gridDim.x == 1;
     if (sh.G > 64) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (sh.lane + j * sh.G) * V;
-            if (c < a.width) store_v<EVEN>(mine, c, a.width, dw[j]);
+            if (c < a.width) put<EVEN>(mine, c, a.width, dw[j], add);
         }
         return;
     }
@@ -252,7 +253,7 @@ __global__ __launch_bounds__(kBlock) void norm_bwd_kernel(BwdArgs a) {
     for (int c = threadIdx.x; c < a.width; c += kBlock) {
         float v = 0.f;
         for (int k = 0; k < kBlock / 64; ++k) v += per_wave[k * a.width + c];
-        mine[c] = v;
+        mine[c] = add ? v + mine[c] : v;
     }
 }
 
@@ -285,8 +286,9 @@ Plan plan(const rgnn_norm_desc_t* d) {
     while (p.G < vectors && p.G < 64) p.G *= 2;
     if (vectors > 4 * 64) p.G = kBlock;
     p.NV = (vectors + p.G - 1) / p.G;
-    const int64_t per_block = kBlock / p.G;
-    p.blocks = (int)std::min<int64_t>(kMaxBlocks, (d->rows + per_block - 1) / per_block);
+    // (what two turns of a workgroup finish is left to one: the backward then needs no second launch)
+    const int64_t turns = (d->rows + kBlock / p.G - 1) / (kBlock / p.G);
+    p.blocks = turns <= 2 ? (int)std::min<int64_t>(turns, 1) : (int)std::min<int64_t>(kMaxBlocks, turns);
     return p;
 }
 
@@ -401,11 +403,11 @@ extern "C" rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void*
             RGNN_FAIL(RGNN_EINVAL, "dWeight overlaps an input or the workspace");
         if (dX || dResidual || dWeight) {
             const BwdArgs a{desc->rows, desc->width, p.G, accumulate, desc->eps, sum, weight, dOut, dSum, dX, dResidual,
-                            dWeight ? static_cast<float*>(workspace) : nullptr};
+                            dWeight ? p.blocks == 1 ? dWeight : static_cast<float*>(workspace) : nullptr};
             RGNN_TRY(with_types(desc, [&](auto tx, auto ts, auto to) { return launch_bwd<decltype(tx), decltype(ts), decltype(to)>(desc, p, a, st); }));
         }
     }
-    if (dWeight && (desc->rows > 0 || !accumulate)) {
+    if (dWeight && p.blocks != 1 && (desc->rows > 0 || !accumulate)) {
         KernelTimer timer(st, "norm_bwd.reduce");
         norm_dw_kernel<<<(desc->width + 15) / 16, 1024, 0, st>>>(static_cast<const float*>(workspace), p.blocks, desc->width, dWeight, accumulate);
         RGNN_CHECK_LAUNCH();

@@ -135,10 +135,10 @@ def test_in_place_and_repeatable():
         assert torch.equal(a, b)
 
 
-def test_accumulate_and_optional_results():
+@pytest.mark.parametrize("rows,width", [(515, 96), (20, 96), (2, 5000), (7, 4099)])
+def test_accumulate_and_optional_results(rows, width):
     import torch
     from paper_2412_04747_amd import binding as B
-    rows, width = 515, 96
     for x, total in (("f32", "f32"), ("bf16", "f32")):
         d = _inputs(rows, width, x, total, "bf16", True, 11)
         L = _layer(d, rows, width, x, total, "bf16", True)
