@@ -7,6 +7,8 @@
 // next product: what an instruction leaves in a lane (the values of one column at rows 8 (i / 4) + 4 (lane / 32) + i % 4, i = 0 .. 15)
 // is, eight by eight, what the next one reads from that lane, if the other operand takes its hidden indices in the same order.
 #pragma once
+#include <math.h>
+
 #include "row_ops.h"
 
 namespace rgnn {
@@ -218,6 +220,14 @@ __device__ __forceinline__ void combine_block(const float* part, int splits, int
 
 // hidden values of a workgroup that forms the weights' gradients
 inline int ffn_grad_columns(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }
+
+// Shares of the rows for them.  A share costs its sums of 3 d f fp32 written and read, 24 d f bytes at some 5 TB/s; a unit of 32 rows takes a
+// workgroup 0.016 d us (fp32: 0.04 d).  With n units the sum of both is least at sqrt(3333 n / f) shares (8333); `most` fill the GPU.
+inline int ffn_grad_shares(const rgnn_ffn_desc_t* d, int most) {
+    const int64_t units = (d->rows + 31) / 32;
+    const double best = sqrt((d->dtype == RGNN_BF16 ? 3333.0 : 8333.0) * (double)units / d->hidden);
+    return (int)std::min<int64_t>(std::min<int64_t>(most, units), std::max(1, (int)best));
+}
 
 // ffn_few.hip: the same for few rows
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward);

@@ -142,11 +142,8 @@ int row_splits(const rgnn_ffn_desc_t* d) {
     return chunks_of(d) <= 3 ? 1 : std::max(1, std::min(chunks_of(d), 256 / std::max(row_blocks(d), 1)));
 }
 int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + ffn_grad_columns(d) - 1) / ffn_grad_columns(d); }
-// Units of 32 rows: one or two need no division.
-int grad_splits(const rgnn_ffn_desc_t* d) {
-    const int units = (int)((d->rows + UNIT - 1) / UNIT);
-    return units <= 2 ? 1 : std::max(1, std::min(units, 256 / grad_groups(d)));
-}
+// (one or two units of 32 rows need no division)
+int grad_splits(const rgnn_ffn_desc_t* d) { return d->rows <= 2 * UNIT ? 1 : ffn_grad_shares(d, std::max(1, 256 / grad_groups(d))); }
 size_t share_bytes(const rgnn_ffn_desc_t* d) {
     const int s = row_splits(d);
     return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
@@ -170,16 +167,16 @@ rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs
 }  // namespace
 
 // Up to which number of rows this is faster than laying out the weights first, in us here / there:
-//   forward   d 32, f 64, bf16: 32000 rows 4.9 / 5.7; fp32: 32000 7.8 / 8.9
-//             d 64, f 256, bf16: 2000 8.3 / 9.4, 4000 10.5 / 9.4; fp32: 12000 19.9 / 20.7, 16000 21.8 / 20.8
-//             d 128, f 341, bf16: 2000 14.3 / 14.2, 4000 18.0 / 14.4; fp32: 12000 41.4 / 44.1, 24000 57.0 / 46.1
-//   backward  d 32, f 64, bf16: 32000 15.4 / 19.9; fp32: 32000 20.1 / 26.1
-//             d 64, f 256, bf16: 3000 24.0 / 24.2, 4000 29.7 / 26.9; fp32: 8000 38.8 / 45.1, 12000 51.9 / 45.3
-//             d 128, f 341, bf16: 4000 35.0 / 35.7, 6000 39.7 / 37.0; fp32: 8000 81.5 / 89.0, 12000 120 / 110
+//   forward   d 32, f 64, bf16: 32000 rows 4.9 / 5.6; fp32: 32000 7.9 / 8.8
+//             d 64, f 256, bf16: 300 6.7 / 7.1, 2000 8.3 / 7.3; fp32: 2000 11.0 / 12.2, 4000 13.8 / 12.3
+//             d 128, f 341, bf16: 300 9.9 / 11.5, 2000 14.2 / 11.8; fp32: 8000 29.5 / 31.3, 12000 41.5 / 31.8
+//   backward  d 32, f 64, bf16: 32000 16.2 / 16.6; fp32: 32000 20.1 / 26.9
+//             d 64, f 256, bf16: 2000 15.2 / 18.3, 4000 24.0 / 19.6; fp32: 8000 39.8 / 42.6, 12000 52.7 / 43.4
+//             d 128, f 341, bf16: 2000 28.7 / 31.3, 4000 35.8 / 33.5; fp32: 8000 81.3 / 87.6, 12000 121 / 109
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
     if (d->width == 32) return d->rows <= 32768;
-    if (d->dtype == RGNN_F32) return d->rows <= (backward ? 8192 : 12288);
-    return d->rows <= (backward ? 3584 : 2304);
+    if (d->dtype == RGNN_F32) return d->rows <= (backward || d->width == 128 ? 8192 : 2560);
+    return d->rows <= (backward ? 2560 : 1024);
 }
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d) + (backward ? grad_bytes(d) : 0)); }
 

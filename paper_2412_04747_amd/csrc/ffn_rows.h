@@ -4,14 +4,14 @@
 
 namespace rgnn {
 
-// N operands from memory into the LDS, by all wavefronts of the workgroup
-template <int N>
+// N operands from memory into the LDS, by WAVES wavefronts
+template <int N, int WAVES>
 __device__ __forceinline__ void fetch(const unsigned char* from, unsigned char* lds) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & (WAVES - 1);
 #pragma unroll
-    for (int i = 0; i < (N + kRowWaves - 1) / kRowWaves; ++i) {
-        const int k = i * kRowWaves + wave;
-        if (N % kRowWaves == 0 || k < N)
+    for (int i = 0; i < (N + WAVES - 1) / WAVES; ++i) {
+        const int k = i * WAVES + wave;
+        if (N % WAVES == 0 || k < N)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(from + (size_t)k * kFrag + lane * 16),
                                              (__attribute__((address_space(3))) void*)(lds + k * kFrag), 16, 0, 0);
     }
@@ -38,24 +38,28 @@ template <int D, int PL, bool BWD> struct RowsCut {
     static constexpr int depth = PL == 1 ? (BWD ? 3 : 4) : 2;     // steps of the second products that an operand is read ahead, and one
 };
 
-// 128 rows, all chunks.
-template <int D, int PL, int ACT, bool BWD>
+// 128 rows, all chunks.  GROUPS > 1: 128 / GROUPS rows, whose chunks are divided among the groups of wavefronts, each with places in the LDS of its own; the
+// shares are added through the LDS, in order.
+template <int D, int PL, int ACT, bool BWD, int GROUPS = 1>
 __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, unsigned char* lds) {
     using W = Weights<D, PL, BWD>;
     using Cut = RowsCut<D, PL, BWD>;
     constexpr int S = D / 16, TILES = D / 32;
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
-    const int64_t row = (block * kRowWaves + wave) * 32 + m;
-    const int c1 = r.a.chunks;
-    auto first = [&](int c) { return lds + (W::twice ? (c & 1) * (W::first + W::second) * kFrag : 0); };
+    constexpr int WAVES = kRowWaves / GROUPS;
+    const int wave = (threadIdx.x >> 6) & (WAVES - 1), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
+    const int group = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / WAVES : 0;
+    const int64_t row = (block * WAVES + wave) * 32 + m;
+    const int c0 = GROUPS > 1 ? r.a.chunks * group / GROUPS : 0, c1 = GROUPS > 1 ? r.a.chunks * (group + 1) / GROUPS : r.a.chunks;
+    unsigned char* const mine = lds + group * W::lds;
+    auto first = [&](int c) { return mine + (W::twice ? (c & 1) * (W::first + W::second) * kFrag : 0); };
     auto second = [&](int c) { return first(c) + W::first * kFrag; };
-    auto fetch_first = [&](int c) { if (c < c1) fetch<W::first>(r.packed + (size_t)c * (W::first + W::second) * kFrag, first(c)); };
-    auto fetch_second = [&](int c) { if (c < c1) fetch<W::second>(r.packed + ((size_t)c * (W::first + W::second) + W::first) * kFrag, second(c)); };
-    fetch_first(0);
+    auto fetch_first = [&](int c) { if (c < c1) fetch<W::first, WAVES>(r.packed + (size_t)c * (W::first + W::second) * kFrag, first(c)); };
+    auto fetch_second = [&](int c) { if (c < c1) fetch<W::second, WAVES>(r.packed + ((size_t)c * (W::first + W::second) + W::first) * kFrag, second(c)); };
+    fetch_first(c0);
     if (W::twice) {
-        if (Cut::ahead) fetch_first(1);
-        fetch_second(0);
+        if (Cut::ahead) fetch_first(c0 + 1);
+        fetch_second(c0);
     }
     bf16x8 x[S][PL], dy[BWD ? S : 1][PL];
     v16f y[TILES];
@@ -167,15 +171,15 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
         none(a);
         arrived();
 #pragma unroll
-        for (int s = 0; s < S; ++s) form(read_first(first(0), s), s, a);
+        for (int s = 0; s < S; ++s) form(read_first(first(c0), s), s, a);
         if (!W::twice) {
             __syncthreads();
-            fetch_first(1);
+            fetch_first(c0 + 1);
         }
         // (two at a time: the sets of hidden values change places without being moved)
         constexpr std::true_type more;
         constexpr std::false_type last;
-        int c = 0;
+        int c = c0;
         for (; c + 2 < c1; c += 2) {
             chunk(more, c, a, b);
             chunk(more, c + 1, b, a);
@@ -187,7 +191,7 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
             chunk(last, c, a, b);
         }
     } else {
-        for (int c = 0; c < c1; ++c) {
+        for (int c = c0; c < c1; ++c) {
             arrived();
             if (W::twice) {
                 fetch_first(c + 1);
@@ -217,6 +221,29 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
             for (int j = 0; j < 16; ++j) activate<ACT>(a, j, v[j], v2[j]);
             result(c, early, v, v2);
         }
+    }
+    if constexpr (GROUPS > 1) {
+        // the groups' numbers of chunks differ by one at most: as many barriers for all
+        if (c1 - c0 < (r.a.chunks + GROUPS - 1) / GROUPS) {
+            arrived();
+            if (!W::twice) arrived();
+        }
+        static_assert((GROUPS - 1) * WAVES * TILES * 16 * 256 <= GROUPS * W::lds, "the shares fit the weights' places");
+        auto share = [&](int g) { return reinterpret_cast<float*>(lds) + ((g - 1) * WAVES + wave) * TILES * 16 * 64 + lane; };
+        __syncthreads();
+        if (group > 0) {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) share(group)[(t * 16 + i) * 64] = y[t][i];
+        }
+        __syncthreads();
+        if (group > 0) return;
+        for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) y[t][i] += share(g)[(t * 16 + i) * 64];
     }
     store_result<D, PL>(r, 0, row, kh, y);
 }

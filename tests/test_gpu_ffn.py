@@ -120,10 +120,12 @@ def test_against_the_definition(rows, width, hidden, dtype, act):
         _check(v, want[k], k)
 
 
-@pytest.mark.parametrize("rows,width,hidden,dtype", [(70001, 128, 40, "bf16"), (70001, 64, 96, "bf16"), (70001, 32, 200, "bf16"), (40003, 64, 70, "f32"),
+@pytest.mark.parametrize("rows,width,hidden,dtype", [(3001, 64, 130, "bf16"), (9001, 64, 33, "bf16"), (9001, 64, 200, "bf16"), (3001, 128, 40, "bf16"),
+                                                     (5003, 64, 97, "f32"), (12001, 64, 90, "f32"), (9003, 128, 65, "f32"), (33001, 32, 97, "f32"),
+                                                     (70001, 128, 40, "bf16"), (70001, 64, 96, "bf16"), (70001, 32, 200, "bf16"), (40003, 64, 70, "f32"),
                                                      (40003, 128, 33, "f32")])
 def test_many_rows(rows, width, hidden, dtype):
-    """Sizes at which the wavefronts take more rows and nothing is split."""
+    """Sizes at which the weights are laid out first: chunks divided among four, two and one group of wavefronts, in even and uneven numbers."""
     import torch
     print(f"ffn case rows={rows} width={width} hidden={hidden} {dtype}", flush=True)
     p = _inputs(rows, width, hidden, dtype, "silu", 3)
