@@ -31,7 +31,9 @@ template <int D, int PL, bool BWD> struct Weights {
 };
 
 // Wavefronts that share a SIMD, and whether the products of chunk c + 1 are issued between the activations of chunk c (the matrix unit and
-// the vector unit then work at the same time within a wavefront, which takes the registers of a second set of hidden values).
+// the vector unit then work at the same time within a wavefront, which takes the registers of a second set of hidden values).  A second wavefront per
+// SIMD is worth more where the registers allow only one of both: backward, 1M rows, d 64, f 256, fp32, this pass 965 us with one wavefront and the
+// second set, 830 with two and without.
 template <int D, int PL, bool BWD> struct RowsCut {
     static constexpr int per_simd = D == 128 && PL == 3 && BWD ? 1 : 2;
     static constexpr bool ahead = !((BWD && (D == 128 || PL == 3)) || (D == 128 && PL == 3));
@@ -73,7 +75,7 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
 
     // Operands are read from the LDS a step before they are multiplied.  The compiler would move the reads to their use and wait there; the
     // backward, whose registers are full, is left to it (2M rows, d 128, f 512, bf16, forward: 935 us without the fences, 913 with;
-    // 200017 rows, f 341, backward: 119 and 134).
+    // 200017 rows, f 341, this pass of the backward: 119 and 134).
     auto fence = [] { if constexpr (!BWD) __builtin_amdgcn_sched_barrier(0); };
     struct FirstOps { bf16x8 f[BWD ? 3 : 2][PL]; };
     struct SecondOps { bf16x8 f[BWD ? 2 : 1][PL]; };
@@ -95,7 +97,7 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
         mul_add<PL>(o.f[1], x[s], h.u);
         if constexpr (BWD) mul_add<PL>(o.f[2], dy[s], h.dh);
     };
-    // early: the operands of the first steps are on their way already
+    // Chunk c's share of the result, from act(g) u (dg and du) in v (and v2).  o: operands of the first steps, on their way already.
     constexpr int DEPTH = Cut::depth < S ? Cut::depth : S;
     auto result = [&](int c, SecondOps (&o)[DEPTH], const float (&v)[16], const float (&v2)[16]) {
         bf16x8 p[2][PL], p2[2][PL];
