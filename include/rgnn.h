@@ -385,7 +385,7 @@ rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const
  *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: every gradient is added to)
  * RGNN_F32: products are formed from three bfloat16 planes per operand on the matrix cores, as close to 64 bits as fp32
  * products are; operands below 2^-110 lose their last bits, and those above 3.38e38 count as infinite.  RGNN_BF16: act(g) u and the gradients of g and u are rounded
- * to bfloat16 where they enter the next product.  An infinite or NaN entry, or a product that leaves the range of fp32, makes its row
+ * to bfloat16 where they enter the next product (with few rows to 16 bits).  An infinite or NaN entry, or a product that leaves the range of fp32, makes its row
  * of out (dX), and the weights' gradients, NaN or infinite; the other rows are not touched by it. */
 typedef struct {
     int64_t rows;                /* up to 2000000000 */

@@ -19,13 +19,18 @@ typedef unsigned rgnn_v2u __attribute__((ext_vector_type(2)));
 
 constexpr int kHid = 32;                 // hidden values of a chunk
 
+// Planes in which act(g) u, dg and du enter the next product.  bf16: one, so that they are rounded to bfloat16 there (with the rounding of the
+// result, an error of 2.3e-3 where one rounding makes 1.7e-3; a second plane would be a third more matrix instructions and the vector ones to
+// split); but two with few rows, where launches are the time and an output of few values may be twice as far off by chance.
+constexpr int hidden_planes(int planes, bool few) { return planes == 1 && few ? 2 : planes; }
+
 struct FfnArgs {
     int64_t rows;
     int hidden, chunks;                  // chunks = ceil(hidden / kHid)
     const void* X; const void* Wg; const void* Wu; const void* Wd; const void* dOut;
 };
 
-// planes of eight values: PL == 1 rounds to bfloat16; PL == 3 is exact to 24 bits, x = hi + mid + lo (each rounded to nearest even)
+// planes of eight values: PL == 1 rounds to bfloat16; PL == 2 keeps 16 bits, PL == 3 is exact to 24: x = hi + mid + lo (each rounded to nearest even)
 template <int PL>
 __device__ __forceinline__ void planes8(const float (&x)[8], bf16x8 (&p)[PL]) {
     rgnn_v4u q[PL];
@@ -49,20 +54,20 @@ __device__ __forceinline__ void planes8(const float (&x)[8], bf16x8 (&p)[PL]) {
 __device__ __forceinline__ v16f mfma(bf16x8 a, bf16x8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ v4f mfma(bf16x8 a, bf16x8 b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
-// c += a b.  Three planes: the six products down to 2^-18 of the largest, small ones first; what is left out is below 2^-26, a quarter
-// of a rounding of the fp32 product.
-template <int PL, typename Acc>
-__device__ __forceinline__ void mul_add(const bf16x8 (&a)[PL], const bf16x8 (&b)[PL], Acc& c) {
-    if constexpr (PL == 1) {
-        c = mfma(a[0], b[0], c);
-    } else {
-        c = mfma(a[0], b[2], c);
-        c = mfma(a[2], b[0], c);
-        c = mfma(a[1], b[1], c);
-        c = mfma(a[0], b[1], c);
-        c = mfma(a[1], b[0], c);
-        c = mfma(a[0], b[0], c);
-    }
+// c += a b.  Three planes of both: the six products down to 2^-18 of the largest, small ones first; what is left out is below 2^-26, a quarter
+// of a rounding of the fp32 product.  One plane and two: both products.
+template <typename Acc>
+__device__ __forceinline__ void mul_add(const bf16x8 (&a)[1], const bf16x8 (&b)[1], Acc& c) { c = mfma(a[0], b[0], c); }
+template <typename Acc>
+__device__ __forceinline__ void mul_add(const bf16x8 (&a)[1], const bf16x8 (&b)[2], Acc& c) { c = mfma(a[0], b[0], mfma(a[0], b[1], c)); }
+template <typename Acc>
+__device__ __forceinline__ void mul_add(const bf16x8 (&a)[3], const bf16x8 (&b)[3], Acc& c) {
+    c = mfma(a[0], b[2], c);
+    c = mfma(a[2], b[0], c);
+    c = mfma(a[1], b[1], c);
+    c = mfma(a[0], b[1], c);
+    c = mfma(a[1], b[0], c);
+    c = mfma(a[0], b[0], c);
 }
 template <typename Acc>
 __device__ __forceinline__ void clear(Acc& c) {

@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, true>::per_simd)) v
     extern __shared__ unsigned char lds[];
     const int b = (int)blockIdx.x - row_blocks;
     if (b < 0) rows_block<D, PL, ACT, true>(r, blockIdx.x, lds);
-    else grad_block<D, PL, ACT, false>(k, b % k.splits, b / k.splits, lds);
+    else grad_block<D, PL, ACT, false, false>(k, b % k.splits, b / k.splits, lds);
 }
 
 template <typename T>

@@ -22,7 +22,7 @@ template <int D, int PL, bool BWD> constexpr int rows_lds() { return (BWD ? 5 : 
 // 128 rows, a share of the chunks.
 template <int D, int PL, int ACT, bool BWD>
 __device__ __forceinline__ void few_rows_block(const RowsArgs& r, int block, int split, unsigned char* lds) {
-    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves;
+    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves, HP = hidden_planes(PL, true);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
     const int64_t row0 = ((int64_t)block * kRowWaves + wave) * 32, row = row0 + m;
@@ -74,12 +74,12 @@ __device__ __forceinline__ void few_rows_block(const RowsArgs& r, int block, int
         for (int s = 0; s < S; ++s) {
             bf16x8 f[PL];
             operand(lds + s * PL * kFrag, f);
-            mul_add<PL>(f, x[s], h.g);
+            mul_add(f, x[s], h.g);
             operand(lds + (S + s) * PL * kFrag, f);
-            mul_add<PL>(f, x[s], h.u);
+            mul_add(f, x[s], h.u);
             if constexpr (BWD) {
                 operand(lds + (2 * S + s) * PL * kFrag, f);
-                mul_add<PL>(f, dy[s], h.dh);
+                mul_add(f, dy[s], h.dh);
             }
         }
         const unsigned char* const w = lds + (BWD ? 3 : 2) * S * PL * kFrag;
@@ -88,16 +88,16 @@ __device__ __forceinline__ void few_rows_block(const RowsArgs& r, int block, int
             float v[8], v2[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) activate<ACT>(h, 8 * s + j, v[j], v2[j]);
-            bf16x8 p[PL], p2[PL], f[PL];
-            planes8<PL>(v, p);
-            if constexpr (BWD) planes8<PL>(v2, p2);
+            bf16x8 p[HP], p2[HP], f[PL];
+            planes8<HP>(v, p);
+            if constexpr (BWD) planes8<HP>(v2, p2);
 #pragma unroll
             for (int t = 0; t < TILES; ++t) {
                 operand(w + (2 * t + s) * PL * kFrag, f);
-                mul_add<PL>(f, p, y[t]);
+                mul_add(f, p, y[t]);
                 if constexpr (BWD) {
                     operand(w + (S + 2 * t + s) * PL * kFrag, f);
-                    mul_add<PL>(f, p2, y[t]);
+                    mul_add(f, p2, y[t]);
                 }
             }
         }
@@ -119,9 +119,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_bwd_kernel(RowsArgs
     if (b < n) {
         few_rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
     } else if (k.splits == 1) {
-        grad_block<D, PL, ACT, true>(k, 0, b - n, lds);
+        grad_block<D, PL, ACT, true, true>(k, 0, b - n, lds);
     } else {
-        grad_block<D, PL, ACT, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
+        grad_block<D, PL, ACT, true, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
     }
 }
 
@@ -167,15 +167,16 @@ rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs
 }  // namespace
 
 // Up to which number of rows this is faster than laying out the weights first, in us here / there:
-//   forward   d 32, f 64, bf16: 32000 rows 4.9 / 5.6; fp32: 32000 7.9 / 8.8
-//             d 64, f 256, bf16: 300 6.7 / 7.1, 2000 8.3 / 7.3; fp32: 2000 11.0 / 12.2, 4000 13.8 / 12.3
-//             d 128, f 341, bf16: 300 9.9 / 11.5, 2000 14.2 / 11.8; fp32: 8000 29.5 / 31.3, 12000 41.5 / 31.8
-//   backward  d 32, f 64, bf16: 32000 16.2 / 16.6; fp32: 32000 20.1 / 26.9
-//             d 64, f 256, bf16: 2000 15.2 / 18.3, 4000 24.0 / 19.6; fp32: 8000 39.8 / 42.6, 12000 52.7 / 43.4
-//             d 128, f 341, bf16: 2000 28.7 / 31.3, 4000 35.8 / 33.5; fp32: 8000 81.3 / 87.6, 12000 121 / 109
+//   forward   d 32, f 64, bf16: 32000 rows 5.1 / 5.6; fp32: 32000 7.9 / 8.8
+//             d 64, f 256, bf16: 300 6.8 / 7.1, 2000 8.3 / 7.3; fp32: 2000 11.0 / 12.2, 4000 13.8 / 12.3
+//             d 128, f 341, bf16: 300 10.0 / 11.5, 2000 14.2 / 11.8; fp32: 8000 29.5 / 31.3, 12000 41.5 / 31.8
+//   backward  d 32, f 64, bf16: 12000 11.6 / 12.7, 24000 16.0 / 15.2; fp32: 32000 20.1 / 26.9
+//             d 64, f 256, bf16: 2000 16.7 / 18.3, 4000 24.0 / 19.6; fp32: 8000 39.8 / 42.6, 12000 52.7 / 43.4
+//             d 128, f 341, bf16: 2000 30.8 / 31.3, 4000 35.8 / 33.5; fp32: 8000 81.3 / 87.6, 12000 121 / 109
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
-    if (d->width == 32) return d->rows <= 32768;
-    if (d->dtype == RGNN_F32) return d->rows <= (backward || d->width == 128 ? 8192 : 2560);
+    const bool f32 = d->dtype == RGNN_F32;
+    if (d->width == 32) return d->rows <= (f32 || !backward ? 32768 : 16384);
+    if (f32) return d->rows <= (backward || d->width == 128 ? 8192 : 2560);
     return d->rows <= (backward ? 2560 : 1024);
 }
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d) + (backward ? grad_bytes(d) : 0)); }

@@ -37,9 +37,9 @@ __device__ __forceinline__ int swizzle(int r) {
 }
 
 // The workgroup's share of the rows, `split`, and of the hidden values, `group`.
-template <int D, int PL, int ACT, bool DIRECT>
+template <int D, int PL, int ACT, bool FEW, bool DIRECT>
 __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int group, unsigned char* lds) {
-    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves;
+    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves, HP = hidden_planes(PL, FEW);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     using Acc = typename std::conditional<MT == 32, v16f, v4f>::type;
     constexpr int KS = MT == 32 ? 16 : 32;               // contraction of an instruction
@@ -160,13 +160,13 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
             for (int s = 0; s < S; ++s) {
                 bf16x8 f[PL];
                 rows_operand(buf, ra, 0, i, s, f);
-                mul_add<PL>(f, wg[s], g[i]);
-                mul_add<PL>(f, wu[s], up[i]);
+                mul_add(f, wg[s], g[i]);
+                mul_add(f, wu[s], up[i]);
                 rows_operand(buf, ra, 1, i, s, f);
-                mul_add<PL>(f, wd[s], dh[i]);
+                mul_add(f, wd[s], dh[i]);
             }
         }
-        bf16x8 hp[STEPS][PL], gp[STEPS][PL], upp[STEPS][PL];
+        bf16x8 hp[STEPS][HP], gp[STEPS][HP], upp[STEPS][HP];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             float vh[8], vg[8], vu[8];
@@ -179,9 +179,9 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
                 vg[j] = dh[i][e] * up[i][e] * slope;
                 vu[j] = dh[i][e] * av;
             }
-            planes8<PL>(vh, hp[s]);
-            planes8<PL>(vg, gp[s]);
-            planes8<PL>(vu, upp[s]);
+            planes8<HP>(vh, hp[s]);
+            planes8<HP>(vg, gp[s]);
+            planes8<HP>(vu, upp[s]);
         }
         // Three planes: the unit's products are summed on their own and then added, one rounding at the gradient's magnitude per 32 rows.
 #pragma unroll
@@ -191,10 +191,10 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
                 for (int s = 0; s < STEPS; ++s) {
                     bf16x8 f[PL];
                     cols_operand(buf, ca, 0, t, s, f);
-                    mul_add<PL>(f, gp[s], dwg[t]);
-                    mul_add<PL>(f, upp[s], dwu[t]);
+                    mul_add(f, gp[s], dwg[t]);
+                    mul_add(f, upp[s], dwu[t]);
                     cols_operand(buf, ca, 1, t, s, f);
-                    mul_add<PL>(f, hp[s], dwd[t]);
+                    mul_add(f, hp[s], dwd[t]);
                 }
             } else {
                 Acc tg, tu, td;
@@ -205,10 +205,10 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
                 for (int s = 0; s < STEPS; ++s) {
                     bf16x8 f[PL];
                     cols_operand(buf, ca, 0, t, s, f);
-                    mul_add<PL>(f, gp[s], tg);
-                    mul_add<PL>(f, upp[s], tu);
+                    mul_add(f, gp[s], tg);
+                    mul_add(f, upp[s], tu);
                     cols_operand(buf, ca, 1, t, s, f);
-                    mul_add<PL>(f, hp[s], td);
+                    mul_add(f, hp[s], td);
                 }
 #pragma unroll
                 for (int e = 0; e < NR; ++e) {

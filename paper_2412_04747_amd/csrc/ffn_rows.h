@@ -93,9 +93,9 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
     };
     // the s-th sixteen columns' share of the chunk's hidden values
     auto form = [&](const FirstOps& o, int s, Hidden<BWD>& h) {
-        mul_add<PL>(o.f[0], x[s], h.g);
-        mul_add<PL>(o.f[1], x[s], h.u);
-        if constexpr (BWD) mul_add<PL>(o.f[2], dy[s], h.dh);
+        mul_add(o.f[0], x[s], h.g);
+        mul_add(o.f[1], x[s], h.u);
+        if constexpr (BWD) mul_add(o.f[2], dy[s], h.dh);
     };
     // Chunk c's share of the result, from act(g) u (dg and du) in v (and v2).  o: operands of the first steps, on their way already.
     constexpr int DEPTH = Cut::depth < S ? Cut::depth : S;
@@ -111,8 +111,8 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
             if (q + DEPTH - 1 < S) o[(q + DEPTH - 1) % DEPTH] = read_second(second(c), q + DEPTH - 1);
             fence();
             const int s = q / TILES, t = q % TILES;
-            mul_add<PL>(o[q % DEPTH].f[0], p[s], y[t]);
-            if constexpr (BWD) mul_add<PL>(o[q % DEPTH].f[1], p2[s], y[t]);
+            mul_add(o[q % DEPTH].f[0], p[s], y[t]);
+            if constexpr (BWD) mul_add(o[q % DEPTH].f[1], p2[s], y[t]);
             if (q == 0) round(1);
             fence();
         }

@@ -160,10 +160,11 @@ rgnn_status_t plan(int64_t count, const int64_t* sizes, Plan* p) {
 }
 
 // Every written range against all others, in order of address.  Reads may share memory among themselves.
-rgnn_status_t check_overlaps(int64_t count, const void* const* grads, void* const* clipped, const int64_t* sizes, const int32_t* dtypes, const float* norm) {
+rgnn_status_t check_overlaps(int64_t count, const void* const* grads, void* const* clipped, const int64_t* sizes, const int32_t* dtypes, const float* norm,
+                             const void* workspace, size_t workspace_bytes) {
     struct R { const char *beg, *end; bool written; int64_t i; };
     std::vector<R> r;
-    r.reserve(2 * count + 1);
+    r.reserve(2 * count + 2);
     auto add = [&](const void* p, size_t n, bool w, int64_t i) { r.push_back({static_cast<const char*>(p), static_cast<const char*>(p) + n, w, i}); };
     for (int64_t i = 0; i < count; ++i) {
         if (sizes[i] == 0) continue;
@@ -172,12 +173,13 @@ rgnn_status_t check_overlaps(int64_t count, const void* const* grads, void* cons
         if (clipped) add(clipped[i], n, true, i);
     }
     add(norm, sizeof(float), true, -1);
+    add(workspace, workspace_bytes, true, -2);
     std::sort(r.begin(), r.end(), [](const R& a, const R& b) { return a.beg < b.beg; });
     const char* any_end = nullptr;           // end of what began before, and of what is written of it
     const char* written_end = nullptr;
     for (const R& x : r) {
         if (x.beg < (x.written ? any_end : written_end))
-            RGNN_FAIL(RGNN_EINVAL, "%s overlaps another tensor", x.i < 0 ? "norm" : x.written ? "a clipped tensor" : "a gradient");
+            RGNN_FAIL(RGNN_EINVAL, "%s overlaps another tensor", x.i == -1 ? "norm" : x.i == -2 ? "the workspace" : x.written ? "a clipped tensor" : "a gradient");
         any_end = std::max(any_end, x.end);
         if (x.written) written_end = std::max(written_end, x.end);
     }
@@ -215,7 +217,7 @@ extern "C" rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* g
         if (at % (dtypes[i] == RGNN_BF16 ? 2 : 4)) RGNN_FAIL(RGNN_EINVAL, "tensor %lld is not aligned to its elements", (long long)i);
     }
     try {
-        RGNN_TRY(check_overlaps(count, grads, clipped, sizes, dtypes, norm));
+        RGNN_TRY(check_overlaps(count, grads, clipped, sizes, dtypes, norm, workspace, sizeof(double) * (size_t)p.pieces));
     } catch (const std::bad_alloc&) {
         RGNN_FAIL(RGNN_ENOMEM, "out of host memory");
     }

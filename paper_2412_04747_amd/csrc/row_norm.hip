@@ -399,8 +399,10 @@ extern "C" rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void*
             if (o.overlaps(ss) || o.overlaps(ws) || o.overlaps(dw) || o.overlaps(wk) || (o.overlaps(ys) && !o.same(ys)) || (o.overlaps(gs) && !o.same(gs)))
                 RGNN_FAIL(RGNN_EINVAL, "dX or dResidual overlaps a tensor that it is not the buffer of");
         if (xs.overlaps(rs)) RGNN_FAIL(RGNN_EINVAL, "dX and dResidual overlap");
-        if (dw.overlaps(ss) || dw.overlaps(ws) || dw.overlaps(ys) || dw.overlaps(gs) || dw.overlaps(wk))
-            RGNN_FAIL(RGNN_EINVAL, "dWeight overlaps an input or the workspace");
+        for (const Span& o : {dw, wk})
+            if (o.overlaps(ss) || o.overlaps(ws) || o.overlaps(ys) || o.overlaps(gs))
+                RGNN_FAIL(RGNN_EINVAL, "dWeight or the workspace overlaps an input");
+        if (dw.overlaps(wk)) RGNN_FAIL(RGNN_EINVAL, "dWeight and the workspace overlap");
         if (dX || dResidual || dWeight) {
             const BwdArgs a{desc->rows, desc->width, p.G, accumulate, desc->eps, sum, weight, dOut, dSum, dX, dResidual,
                             dWeight ? p.blocks == 1 ? dWeight : static_cast<float*>(workspace) : nullptr};

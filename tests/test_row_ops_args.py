@@ -66,6 +66,8 @@ def test_norm_pointers():
     refused(EINVAL, "overlap", bwd, d, A[0], A[1], A[2], None, A[3], A[3], A[4], A[5])
     refused(EINVAL, "dWeight", bwd, d, A[0], A[1], A[2], None, A[3], None, A[2], A[5])
     refused(EINVAL, "aligned", bwd, d, A[0], A[1], A[2], None, A[3], None, A[4], A[5] + 4)
+    refused(EINVAL, "workspace", bwd, d, A[0], A[1], A[2], None, A[3], None, A[4], A[0] + 256)    # workspace over sum
+    refused(EINVAL, "workspace", bwd, d, A[0], A[1], A[2], None, A[3], None, A[4], A[4])          # workspace over dWeight
 
 
 # ---- feed-forward block
@@ -122,6 +124,7 @@ def clip(grads=(A[0], A[1]), clipped=(A[2], A[3]), sizes=(100, 100), dtypes=(0, 
     (dict(clipped=(A[0] + 4, A[3])), EINVAL, "overlaps"),                                # shifted by an element
     (dict(clipped=(A[1], A[0])), EINVAL, "overlaps"),                                    # each over the other's gradient
     (dict(clipped=None, norm=A[1] + 40), EINVAL, "overlaps"),                            # the norm into a gradient
+    (dict(ws=A[1] + 16), EINVAL, "overlaps"), (dict(ws=A[4]), EINVAL, "overlaps"),       # the workspace into a gradient, or the norm
     (dict(grads=(A[0], A[0] + 200), clipped=(A[0], A[0] + 200), dtypes=(0, 1)), EINVAL, "overlaps")])
 def test_clip_refusals(change, status, word):
     refused(status, word, lambda: clip(**change))
