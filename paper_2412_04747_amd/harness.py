@@ -26,7 +26,8 @@ def _buf(nbytes):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    """hipStream_t of the current stream (torch.cuda.current_stream().cuda_stream, without the Stream object: 0.3 us for 2.7)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class Graph:
