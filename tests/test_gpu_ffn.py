@@ -100,7 +100,7 @@ def _check(got, want, what):
     assert n <= m, what
 
 
-CASES = [(1, 32, 1), (1, 128, 512), (2, 64, 33), (31, 64, 31), (33, 32, 32), (127, 128, 65), (129, 64, 86), (300, 128, 341), (1000, 32, 86),
+CASES = [(1, 32, 1), (1, 128, 512), (2, 64, 33), (3, 128, 2500), (4, 32, 97), (4, 64, 300), (5, 128, 70), (31, 64, 31), (33, 32, 32), (127, 128, 65), (129, 64, 86), (300, 128, 341), (1000, 32, 86),
          (1000, 128, 128), (513, 64, 1000), (4099, 64, 256)]
 
 
