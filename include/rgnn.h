@@ -348,7 +348,7 @@ rgnn_status_t rgnn_hgt_bwd(const rgnn_graph_t* g, const rgnn_layer_desc_t* desc,
  * nothing but the zeros of its parameter gradients, and its row tensors may be NULL.
  *
  * Unlike the layers, whose results are fp32 whatever they read, these write the type they name: rows of 2 bytes pass
- * from one operator, or layer, to the next without a conversion.  Sums and products are fp32 in every case, and a
+ * from one operator, or layer, to the next without a conversion.  Sums are fp32 or wider in every case, and a
  * result is rounded once, to nearest even, where it is stored.
  */
 
@@ -384,8 +384,8 @@ rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const
  *   activation RGNN_ACT_SILU (g / (1 + exp(-g))) or RGNN_ACT_RELU (its derivative at 0 is 0)
  *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: every gradient is added to)
  * RGNN_F32: products are formed from three bfloat16 planes per operand on the matrix cores, as close to 64 bits as fp32
- * products are; operands below 2^-110 lose their last bits, and those above 3.38e38 count as infinite.  RGNN_BF16: act(g) u and the gradients of g and u are rounded
- * to bfloat16 where they enter the next product (with few rows to 16 bits).  An infinite or NaN entry, or a product that leaves the range of fp32, makes its row
+ * products are; operands below 2^-110 lose their last bits, and those above 3.38e38 count as infinite.  RGNN_BF16: act(g) u and the gradients of g and u
+ * enter the next product with 16 bits at least, however many rows there are.  An infinite or NaN entry, or a product that leaves the range of fp32, makes its row
  * of out (dX), and the weights' gradients, NaN or infinite; the other rows are not touched by it. */
 typedef struct {
     int64_t rows;                /* up to 2000000000 */

@@ -9,8 +9,8 @@
 //
 // Matrix instructions bound it, 6 N d f operations forward and 16 N d f backward (22 as the hidden values are formed twice), sixfold for fp32;
 // in bf16 up to width 64 the vector instructions, an exponential and a reciprocal per hidden value.  Against 1160 TFLOP/s of a large bf16 product:
-//   forward   2M rows, d 128, f 512, bf16: 832 us, 945 TFLOP/s; 1M rows, d 64, f 256, bf16: 155 us, 630; fp32: 498 us, 1180 of plane products
-//   backward  200017 rows, d 128, f 341, bf16: 237 us, 810 of the 22; 1M rows, d 64, f 256, fp32: 1860 us, 1160 of plane products
+//   forward   2M rows, d 128, f 512, bf16: 1015 us, 775 TFLOP/s (one plane more of h in the last product: 1030 of what is done); 1M rows, d 64, f 256, bf16: 155 us, 630; fp32: 498 us, 1180 of plane products
+//   backward  200017 rows, d 128, f 341, bf16: 311 us, 620 of the 22 (900 of the 32 that the second planes make of them); 1M rows, d 64, f 256, fp32: 1860 us, 1160 of plane products
 #include <math.h>
 
 #include "rgnn_internal.h"
@@ -63,7 +63,7 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, true>::per_simd)) v
     extern __shared__ unsigned char lds[];
     const int b = (int)blockIdx.x - row_blocks;
     if (b < 0) rows_block<D, PL, ACT, true>(r, blockIdx.x, lds);
-    else grad_block<D, PL, ACT, false, false>(k, b % k.splits, b / k.splits, lds);
+    else grad_block<D, PL, ACT, false>(k, b % k.splits, b / k.splits, lds);
 }
 
 template <typename T>

@@ -22,7 +22,7 @@ template <int D, int PL, bool BWD> constexpr int rows_lds() { return (BWD ? 5 : 
 // 128 rows, a share of the chunks.
 template <int D, int PL, int ACT, bool BWD>
 __device__ __forceinline__ void few_rows_block(const RowsArgs& r, int block, int split, unsigned char* lds) {
-    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves, HP = hidden_planes(PL, true);
+    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves, HP = hidden_planes(PL);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
     const int64_t row0 = ((int64_t)block * kRowWaves + wave) * 32, row = row0 + m;
@@ -191,9 +191,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_bwd_kernel(RowsArgs
     if (b < n) {
         few_rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
     } else if (k.splits == 1) {
-        grad_block<D, PL, ACT, true, true>(k, 0, b - n, lds);
+        grad_block<D, PL, ACT, true>(k, 0, b - n, lds);
     } else {
-        grad_block<D, PL, ACT, true, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
+        grad_block<D, PL, ACT, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
     }
 }
 

@@ -37,9 +37,9 @@ __device__ __forceinline__ int swizzle(int r) {
 }
 
 // The workgroup's share of the rows, `split`, and of the hidden values, `group`.
-template <int D, int PL, int ACT, bool FEW, bool DIRECT>
+template <int D, int PL, int ACT, bool DIRECT>
 __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int group, unsigned char* lds) {
-    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves, HP = hidden_planes(PL, FEW);
+    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves, HP = hidden_planes(PL);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     using Acc = typename std::conditional<MT == 32, v16f, v4f>::type;
     constexpr int KS = MT == 32 ? 16 : 32;               // contraction of an instruction

@@ -46,7 +46,7 @@ template <int D, int PL, int ACT, bool BWD, int GROUPS = 1>
 __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, unsigned char* lds) {
     using W = Weights<D, PL, BWD>;
     using Cut = RowsCut<D, PL, BWD>;
-    constexpr int S = D / 16, TILES = D / 32;
+    constexpr int S = D / 16, TILES = D / 32, HP = hidden_planes(PL);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     constexpr int WAVES = kRowWaves / GROUPS;
     const int wave = (threadIdx.x >> 6) & (WAVES - 1), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
@@ -100,10 +100,10 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
     // Chunk c's share of the result, from act(g) u (dg and du) in v (and v2).  o: operands of the first steps, on their way already.
     constexpr int DEPTH = Cut::depth < S ? Cut::depth : S;
     auto result = [&](int c, SecondOps (&o)[DEPTH], const float (&v)[16], const float (&v2)[16]) {
-        bf16x8 p[2][PL], p2[2][PL];
+        bf16x8 p[2][HP], p2[2][HP];
         auto round = [&](int s) {
-            planes8<PL>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
-            if constexpr (BWD) planes8<PL>(*reinterpret_cast<const float(*)[8]>(v2 + 8 * s), p2[s]);
+            planes8<HP>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
+            if constexpr (BWD) planes8<HP>(*reinterpret_cast<const float(*)[8]>(v2 + 8 * s), p2[s]);
         };
         round(0);
 #pragma unroll
