@@ -144,8 +144,13 @@ def _rows(*tensors):
     return [t if t is None else t.contiguous() if t.data_ptr() % 16 == 0 or not t.is_contiguous() else t.clone() for t in tensors]
 
 
+_CODES = {torch.float32: B.RGNN_F32, torch.bfloat16: B.RGNN_BF16}
+
+
 def _code(dtype):
-    return B.RGNN_BF16 if dtype == torch.bfloat16 else B.RGNN_F32
+    if dtype not in _CODES:
+        raise TypeError(f"rgnn row operators take and give fp32 or bf16, not {dtype}")
+    return _CODES[dtype]
 
 
 class _ResidualNorm(torch.autograd.Function):
@@ -221,7 +226,9 @@ class _GatedFfn(torch.autograd.Function):
 
 def residual_norm(x, weight, residual=None, eps=1e-6, out_dtype=None):
     """Residual addition and root-mean-square norm over the last dimension, s = x + residual, out = s / sqrt(mean(s^2) + eps) * weight:
-    (out, s), or out alone without a residual.  s has the residual's type; out has out_dtype (default: x's); weight is fp32."""
+    (out, s), or out alone without a residual.  s has the residual's type; out has out_dtype (fp32 or bf16; default: x's); weight is fp32."""
+    if out_dtype is not None and out_dtype not in _CODES:
+        raise TypeError(f"residual_norm: out_dtype is fp32 or bf16, not {out_dtype}")
     return _ResidualNorm.apply(float(eps), out_dtype or x.dtype, x, residual, weight)
 
 
