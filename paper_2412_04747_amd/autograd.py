@@ -20,7 +20,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
-from .harness import Graph, _buf, _stream
+from .harness import Graph, _buf, _dense, _stream
 
 
 def _bufs(graph, layer, desc, key):
@@ -237,18 +237,6 @@ def gated_ffn(X, Wg, Wu, Wd, act="silu"):
     if act not in ("silu", "relu"):
         raise ValueError(f"gated_ffn: unknown activation {act!r}")
     return _GatedFfn.apply(act, X, Wg, Wu, Wd)
-
-
-def _dense(t):
-    """Whether the tensor's elements fill one stretch of memory, in whatever order."""
-    if t.is_contiguous():
-        return True
-    step = 1
-    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
-        if stride != step:
-            return False
-        step *= size
-    return True
 
 
 @torch.no_grad()

@@ -227,20 +227,49 @@ class FfnLayer:
         return dict(dX=self.dX, dWg=self.dWg, dWu=self.dWu, dWd=self.dWd)
 
 
+def _dense(t):
+    """Whether the tensor's elements fill one stretch of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+_CLIP_TYPES = {torch.float32: B.RGNN_F32, torch.bfloat16: B.RGNN_BF16}
+
+
 class GradClip:
     """The workspace, tables and result buffers for clipping tensors of the sizes and types of `like`, in place or into `clipped`."""
 
     def __init__(self, like, in_place=True):
-        sizes = [t.numel() for t in like]
-        self.ws = _buf(B.rgnn_clip_workspace_bytes(sizes))
-        self.sizes, self.dtypes = B.clip_tables(sizes, [B.RGNN_BF16 if t.dtype == torch.bfloat16 else B.RGNN_F32 for t in like])
+        for t in like:
+            if t.dtype not in _CLIP_TYPES or not t.is_cuda or not _dense(t):
+                raise TypeError(f"GradClip takes dense fp32 or bf16 tensors on the GPU, not {t.dtype} of strides {t.stride()} on {t.device}")
+        self._numel, self._types, self._devices = [t.numel() for t in like], [t.dtype for t in like], [t.get_device() for t in like]
+        # (tensors that are not contiguous are taken by their exact layout)
+        self._layouts = None if all(t.is_contiguous() for t in like) else [(t.shape, t.stride()) for t in like]
+        self.ws = _buf(B.rgnn_clip_workspace_bytes(self._numel))
+        self.sizes, self.dtypes = B.clip_tables(self._numel, [_CLIP_TYPES[t] for t in self._types])
         self.norm = torch.empty((), device="cuda")
         self.clipped = None if in_place else [torch.empty_like(t) for t in like]
         self._to = None if in_place else B.addresses(self.clipped)
 
+    def _check(self, grads):
+        if len(grads) != len(self._numel):
+            raise ValueError(f"GradClip.clip: {len(grads)} tensors, made for {len(self._numel)}")
+        if (list(map(torch.Tensor.numel, grads)) != self._numel or [t.dtype for t in grads] != self._types
+                or list(map(torch.Tensor.get_device, grads)) != self._devices):
+            raise ValueError("GradClip.clip: tensors of other sizes, types or devices than it is made for")
+        if (not all(map(torch.Tensor.is_contiguous, grads)) if self._layouts is None
+                else [(t.shape, t.stride()) for t in grads] != self._layouts):
+            raise ValueError("GradClip.clip: tensors of another layout than it is made for")
+
     def clip(self, grads, max_norm):
-        """`grads`: tensors of the sizes and types of `like`, in its order."""
-        if len(grads) != len(self.sizes):
-            raise ValueError(f"GradClip.clip: {len(grads)} tensors, made for {len(self.sizes)}")
+        """`grads`: tensors of the sizes, types and layouts of `like`, in its order."""
+        self._check(grads)
         given = B.addresses(grads)
         B.rgnn_clip_grad_norm(given, given if self._to is None else self._to, self.sizes, self.dtypes, max_norm, self.norm, self.ws, _stream())
