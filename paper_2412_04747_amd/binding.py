@@ -270,7 +270,11 @@ def rgnn_clip_grad_norm(grads, clipped, sizes, dtypes, max_norm, norm, workspace
     results = None if clipped is None else given if clipped is grads else clipped if isinstance(clipped, C.Array) else addresses(clipped)
     if not isinstance(sizes, C.Array):
         sizes, dtypes = clip_tables(sizes, dtypes)
-    _check(lib().rgnn_clip_grad_norm(len(given), given, results, sizes, dtypes, max_norm, _addr(norm), _addr(workspace), stream))
+    n = len(given)
+    if len(sizes) != n or len(dtypes) != n or (results is not None and len(results) != n):
+        raise ValueError(f"rgnn_clip_grad_norm: {n} tensors, {len(sizes)} sizes, {len(dtypes)} types"
+                         + (f", {len(results)} results" if results is not None else ""))
+    _check(lib().rgnn_clip_grad_norm(n, given, results, sizes, dtypes, max_norm, _addr(norm), _addr(workspace), stream))
 
 
 def rgnn_profile_select(name=None):

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2412_04747_amd import autograd as A
+from paper_2412_04747_amd import binding as B
 from paper_2412_04747_amd import harness as H
 
 
@@ -35,3 +36,12 @@ def test_grad_clip_compares_what_it_is_given():
     for bad in (a, torch.zeros(6)):
         with pytest.raises(ValueError, match="layout"):
             L._check([bad, b])
+
+
+def test_clip_tables_of_one_length():
+    """Raw addresses, never read: the lists' lengths are compared first."""
+    at = [1 << 28, 1 << 29]
+    for grads, clipped, sizes, dtypes in ((at, None, [4], [0, 0]), (at, at, [4, 4], [0]), (at, at[:1], [4, 4], [0, 0]), (at[:1], None, [4, 4], [0, 0]),
+                                          (at, at, *B.clip_tables([4], [0]))):
+        with pytest.raises(ValueError, match="tensors"):
+            B.rgnn_clip_grad_norm(grads, clipped, sizes, dtypes, 1.0, 1 << 30, 1 << 31)
