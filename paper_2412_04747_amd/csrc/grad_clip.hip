@@ -4,7 +4,8 @@
 //
 // Two reads of every gradient and one write: the memory's rate is the bound, and for a small model the two launches.  Every
 // workgroup of the first takes a piece of one tensor and leaves the sum of its squares; every workgroup of the second adds up all those sums
-// itself, in the same order (16 KB at most from the L2, less than a launch in between costs), and scales a piece.
+// itself, in the same order (32 KB at most from the L2, less than a launch in between costs), and scales a piece.  A piece is one tensor's, so that
+// thousands of small tensors are as many pieces: of more than kDirect sums, a launch in between first adds as many at a time.
 // Squares and sums are fp64: 3e38 squared is in range, and a norm over 10^9 terms is right to the last bit of fp32.  That costs nothing: 66M fp32 elements
 // clipped into other memory take 150 us, 5.3 TB/s of two reads and a write, what a copy reaches.
 // The tensors come as a table in the kernel arguments, so that nothing is copied to the device and a captured call keeps its table.
@@ -25,6 +26,7 @@ constexpr int kTable = 128;              // tensors per launch: 3.7 KB of the 4 
 constexpr int kSmallTable = 16;          // of a launch of few, which need not carry them
 constexpr int kPieces = 2048;            // about as many pieces in all: eight workgroups per compute unit
 constexpr int64_t kMinPiece = 4096;      // elements
+constexpr int kDirect = 4096;            // sums that a workgroup adds: 2^24, the most pieces of a call, are 4096 of 4096
 
 template <int N>
 struct Table {
@@ -107,6 +109,15 @@ __global__ __launch_bounds__(kThreads) void grad_squares_kernel(Table<N> t, int6
     if (threadIdx.x == 0) sums[blockIdx.x] = s;
 }
 
+__global__ __launch_bounds__(kThreads) void grad_fold_kernel(const double* sums, int num_sums, double* folded) {
+    __shared__ double lds[kThreads / 64];
+    const int beg = blockIdx.x * kDirect, end = min(beg + kDirect, num_sums);
+    double s = 0.0;
+    for (int i = beg + threadIdx.x; i < end; i += kThreads) s += sums[i];
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) folded[blockIdx.x] = s;
+}
+
 template <typename T>
 __device__ __forceinline__ void scale(const T* g, T* out, int64_t beg, int64_t end, float c) {
     constexpr int V = RowT<T>::V;
@@ -142,7 +153,10 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table<N> t, int64_
 }
 
 // Pieces of the tensors: all of one length, a multiple of 8 elements.
-struct Plan { int64_t piece, pieces; };
+struct Plan {
+    int64_t piece, pieces, folds;        // folds: sums of kDirect pieces' each, 0 where the pieces' are added directly
+    size_t bytes() const { return sizeof(double) * (size_t)(pieces + folds); }
+};
 rgnn_status_t plan(int64_t count, const int64_t* sizes, Plan* p) {
     if (count < 0) RGNN_FAIL(RGNN_EINVAL, "count %lld is negative", (long long)count);
     if (count > 0 && !sizes) RGNN_FAIL(RGNN_EINVAL, "sizes is NULL");
@@ -156,6 +170,7 @@ rgnn_status_t plan(int64_t count, const int64_t* sizes, Plan* p) {
     p->pieces = 0;
     for (int64_t i = 0; i < count; ++i) p->pieces += (sizes[i] + p->piece - 1) / p->piece;
     if (p->pieces > 1 << 24) RGNN_FAIL(RGNN_EUNSUPPORTED, "%lld tensors are too many", (long long)count);
+    p->folds = p->pieces > kDirect ? (p->pieces + kDirect - 1) / kDirect : 0;
     return RGNN_OK;
 }
 
@@ -196,7 +211,7 @@ extern "C" rgnn_status_t rgnn_clip_workspace_bytes(int64_t count, const int64_t*
     Plan p;
     RGNN_TRY(plan(count, sizes, &p));
     if (!workspace) RGNN_FAIL(RGNN_EINVAL, "workspace is NULL");
-    *workspace = align_up(sizeof(double) * (size_t)std::max<int64_t>(p.pieces, 1));
+    *workspace = align_up(std::max(p.bytes(), sizeof(double)));
     return RGNN_OK;
 }
 
@@ -217,7 +232,7 @@ extern "C" rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* g
         if (at % (dtypes[i] == RGNN_BF16 ? 2 : 4)) RGNN_FAIL(RGNN_EINVAL, "tensor %lld is not aligned to its elements", (long long)i);
     }
     try {
-        RGNN_TRY(check_overlaps(count, grads, clipped, sizes, dtypes, norm, workspace, sizeof(double) * (size_t)p.pieces));
+        RGNN_TRY(check_overlaps(count, grads, clipped, sizes, dtypes, norm, workspace, p.bytes()));
     } catch (const std::bad_alloc&) {
         RGNN_FAIL(RGNN_ENOMEM, "out of host memory");
     }
@@ -261,10 +276,19 @@ extern "C" rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* g
         at += blocks;
         return RGNN_OK;
     }));
+    const double* added = sums;
+    int num_added = (int)p.pieces;
+    if (p.folds) {
+        KernelTimer timer(st, "grad_fold");
+        grad_fold_kernel<<<(unsigned)p.folds, kThreads, 0, st>>>(sums, (int)p.pieces, sums + p.pieces);
+        RGNN_CHECK_LAUNCH();
+        added = sums + p.pieces;
+        num_added = (int)p.folds;
+    }
     bool stored = false;
     auto scale_launch = [&](const Table<kTable>& t, int blocks) -> rgnn_status_t {
         KernelTimer timer(st, "grad_scale");
-        fitting(t, [&](const auto& u) { grad_scale_kernel<<<blocks, kThreads, 0, st>>>(u, p.piece, sums, (int)p.pieces, max_norm, stored ? nullptr : norm); });
+        fitting(t, [&](const auto& u) { grad_scale_kernel<<<blocks, kThreads, 0, st>>>(u, p.piece, added, num_added, max_norm, stored ? nullptr : norm); });
         RGNN_CHECK_LAUNCH();
         stored = true;
         return RGNN_OK;
