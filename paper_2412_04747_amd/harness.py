@@ -3,6 +3,8 @@
 They only allocate device buffers with PyTorch, copy inputs in / results out and
 call the C ABI through `binding`; no layer arithmetic happens here.
 """
+import ctypes as C
+
 import numpy as np
 import torch
 
@@ -271,5 +273,5 @@ class GradClip:
     def clip(self, grads, max_norm):
         """`grads`: tensors of the sizes, types and layouts of `like`, in its order."""
         self._check(grads)
-        given = B.addresses(grads)
+        given = (C.c_void_p * len(grads))(*map(torch.Tensor.data_ptr, grads))
         B.rgnn_clip_grad_norm(given, given if self._to is None else self._to, self.sizes, self.dtypes, max_norm, self.norm, self.ws, _stream())
