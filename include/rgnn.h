@@ -356,7 +356,8 @@ rgnn_status_t rgnn_hgt_bwd(const rgnn_graph_t* g, const rgnn_layer_desc_t* desc,
  *   sum = x + residual;   out = sum / sqrt(mean(sum^2) + eps) * weight
  * x_dtype: x, dX.  sum_dtype: residual, sum, dSum, dResidual.  out_dtype: out, dOut.  RGNN_F32 or RGNN_BF16 each: a layer's
  * fp32 rows can be added to a bf16 stream, an fp32 stream be handed to the next layer in bf16.  weight and dWeight are
- * fp32.  The mean of the squares has to be in the range of fp32.
+ * fp32.  Rows of finite sums may be as large as their type allows; with eps = 0 the mean of the squares must not be
+ * below the range of fp32.
  *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: dX, dResidual and dWeight are added to) */
 typedef struct {
     int64_t rows;                /* below 2^31 */
