@@ -411,8 +411,9 @@ rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const voi
  * the call returns.  A pointer needs its element's alignment only; one of an empty tensor may be NULL.  norm: one float on the device.
  * clipped == NULL: the norm alone (max_norm is ignored).  clipped[i] is grads[i] itself (in place) or memory that overlaps nothing
  * else; EINVAL otherwise, also for a tensor that is clipped in place and given twice.
- * Squares and sums are fp64, in a fixed order.  A NaN among the gradients makes the norm and all of `clipped` NaN; an infinite norm makes
- * the finite ones 0; with max_norm = INFINITY nothing is clipped. */
+ * Squares, sums and the coefficient are fp64, in a fixed order; finite gradients whose norm is past fp32 are clipped by it, though `norm` is stored as
+ * infinite.  A NaN among the gradients makes the norm and all of `clipped` NaN; an infinite one makes the norm infinite, the finite ones 0 and itself NaN;
+ * with max_norm = INFINITY nothing is clipped. */
 rgnn_status_t rgnn_clip_workspace_bytes(int64_t count, const int64_t* sizes, size_t* workspace);
 rgnn_status_t rgnn_clip_grad_norm(int64_t count, const void* const* grads, void* const* clipped, const int64_t* sizes,
                                   const int32_t* dtypes, float max_norm, float* norm, void* workspace, void* stream);

@@ -9,6 +9,7 @@
 // Squares and sums are fp64: 3e38 squared is in range, and a norm over 10^9 terms is right to the last bit of fp32.  That costs nothing: 66M fp32 elements
 // clipped into other memory take 150 us, 5.3 TB/s of two reads and a write, what a copy reaches.
 // The tensors come as a table in the kernel arguments, so that nothing is copied to the device and a captured call keeps its table.
+#include <float.h>
 #include <math.h>
 #include <algorithm>
 #include <vector>
@@ -119,7 +120,7 @@ __global__ __launch_bounds__(kThreads) void grad_fold_kernel(const double* sums,
 }
 
 template <typename T>
-__device__ __forceinline__ void scale(const T* g, T* out, int64_t beg, int64_t end, float c) {
+__device__ __forceinline__ void scale(const T* g, T* out, int64_t beg, int64_t end, float c0, float c) {
     constexpr int V = RowT<T>::V;
     for_piece<V>(beg, end, aligned16(g) && aligned16(out), [&](int64_t i, auto n) {
         float v[n()][V];
@@ -128,10 +129,10 @@ __device__ __forceinline__ void scale(const T* g, T* out, int64_t beg, int64_t e
 #pragma unroll
         for (int k = 0; k < n(); ++k) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[k][e] *= c;
+            for (int e = 0; e < V; ++e) v[k][e] = v[k][e] * c0 * c;
             store_cols<V>(out + i + k * kThreads * V, v[k]);
         }
-    }, [&](int64_t i) { out[i] = narrow<T>(widen(g[i]) * c); });
+    }, [&](int64_t i) { out[i] = narrow<T>(widen(g[i]) * c0 * c); });
 }
 
 // Workgroup 0 stores the norm (null in the launches after the first).  t.count == 0: the norm alone.
@@ -148,8 +149,11 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(Table<N> t, int64_
     // last pieces first: they are what the caches still hold of the first pass
     const Piece p = find_piece(t, piece, gridDim.x - 1 - blockIdx.x);
     if (c == 1.0 && p.g == p.out) return;
-    if (p.bf16) scale(static_cast<const bf16_t*>(p.g), static_cast<bf16_t*>(p.out), p.beg, p.end, (float)c);
-    else scale(static_cast<const float*>(p.g), static_cast<float*>(p.out), p.beg, p.end, (float)c);
+    // (a coefficient below fp32's normal range, of a norm up to 2^21 times the largest value, in two factors)
+    const bool low = c > 0.0 && c < FLT_MIN;
+    const float c0 = low ? 0x1p-100f : 1.f, c1 = (float)(low ? c * 0x1p100 : c);
+    if (p.bf16) scale(static_cast<const bf16_t*>(p.g), static_cast<bf16_t*>(p.out), p.beg, p.end, c0, c1);
+    else scale(static_cast<const float*>(p.g), static_cast<float*>(p.out), p.beg, p.end, c0, c1);
 }
 
 // Pieces of the tensors: all of one length, a multiple of 8 elements.
