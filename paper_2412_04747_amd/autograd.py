@@ -239,6 +239,16 @@ def gated_ffn(X, Wg, Wu, Wd, act="silu"):
     return _GatedFfn.apply(act, X, Wg, Wu, Wd)
 
 
+def _apart(t):
+    """Whether no two of the tensor's elements share memory: each stride steps over all that the smaller ones reach."""
+    reach = 0
+    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride <= reach:
+            return t.numel() == 0
+        reach += stride * (size - 1)
+    return True
+
+
 @torch.no_grad()
 def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
     """Scales the gradients of `parameters` in place by min(1, max_norm / (norm + 1e-6)), norm the 2-norm of all of them together, and
@@ -252,6 +262,8 @@ def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
     for g in given:
         if g.layout != torch.strided or g.dtype not in (torch.float32, torch.bfloat16) or not g.is_cuda or g.device != given[0].device:
             raise TypeError("clip_grad_norm_ takes dense fp32 or bf16 gradients on one GPU")
+        if not _apart(g):
+            raise RuntimeError(f"clip_grad_norm_: elements of a gradient share memory (shape {tuple(g.shape)}, strides {g.stride()})")
     with torch.cuda.device(given[0].device):
         grads = [g if _dense(g) else g.contiguous() for g in given]
         sizes = [g.numel() for g in grads]
