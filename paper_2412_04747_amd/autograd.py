@@ -253,7 +253,7 @@ def _apart(t):
 def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
     """Scales the gradients of `parameters` in place by min(1, max_norm / (norm + 1e-6)), norm the 2-norm of all of them together, and
     returns that norm (0-dim fp32 tensor on the GPU; nothing waits for it unless error_if_nonfinite).  Gradients are fp32 or bf16, on one
-    GPU; two that share memory are refused."""
+    GPU; two that share memory are refused (of strided ones, that begin at the same place)."""
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
     given = [p.grad for p in parameters if p.grad is not None]
@@ -265,6 +265,10 @@ def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
         if not _apart(g):
             raise RuntimeError(f"clip_grad_norm_: elements of a gradient share memory (shape {tuple(g.shape)}, strides {g.stride()})")
     with torch.cuda.device(given[0].device):
+        # (strided ones reach the library as copies, whose own memory it compares)
+        strided = [g.data_ptr() for g in given if g.numel() and not _dense(g)]
+        if len(set(strided)) < len(strided):
+            raise RuntimeError("clip_grad_norm_: two gradients share memory")
         grads = [g if _dense(g) else g.contiguous() for g in given]
         sizes = [g.numel() for g in grads]
         norm = torch.empty((), device=given[0].device)

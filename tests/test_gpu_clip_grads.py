@@ -26,3 +26,17 @@ def test_an_expanded_gradient_is_refused_before_anything_is_scaled():
     norm = A.clip_grad_norm_([first, _param(apart), _param(torch.ones(0, 4, device="cuda"))], 1.0)
     want = math.sqrt(15 * 4.0 + 12 * 9.0)
     assert abs(float(norm) - want) < 1e-6 * want and (apart - 3.0 / want).abs().max() < 1e-6
+
+
+def test_strided_gradients_given_twice():
+    from paper_2412_04747_amd import autograd as A
+    view = torch.ones(6, 8, device="cuda")[:, ::2]
+    p = _param(view)
+    for twice in ([p, p], [p, _param(view[:3])]):
+        with pytest.raises(RuntimeError, match="share memory"):
+            A.clip_grad_norm_(twice, 0.1)
+    assert (view == 1.0).all()
+    both = torch.full((6, 8), 2.0, device="cuda")        # columns in turn: neither has an element of the other
+    norm = A.clip_grad_norm_([_param(both[:, ::2]), _param(both[:, 1::2])], 1.0)
+    want = math.sqrt(48 * 4.0)
+    assert abs(float(norm) - want) < 1e-6 * want and (both - 2.0 / want).abs().max() < 1e-6
