@@ -278,6 +278,7 @@ def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
             if not torch.isfinite(norm):
                 raise RuntimeError(f"the norm of the gradients is {norm.item()}, so that they cannot be clipped")
         B.rgnn_clip_grad_norm(grads, grads, sizes, dtypes, float(max_norm), norm, ws, _stream())
+        torch.autograd.graph.increment_version([g for g, c in zip(given, grads) if c is g])
         for g, c in zip(given, grads):
             if c is not g:
                 g.copy_(c)

@@ -40,3 +40,15 @@ def test_strided_gradients_given_twice():
     norm = A.clip_grad_norm_([_param(both[:, ::2]), _param(both[:, 1::2])], 1.0)
     want = math.sqrt(48 * 4.0)
     assert abs(float(norm) - want) < 1e-6 * want and (both - 2.0 / want).abs().max() < 1e-6
+
+
+def test_autograd_sees_that_gradients_changed():
+    """A graph that saved a gradient must not be walked back over the clipped values."""
+    from paper_2412_04747_amd import autograd as A
+    p = torch.nn.Parameter(torch.ones(4, device="cuda"))
+    p.grad = torch.full((4,), 3.0, device="cuda")
+    q = torch.ones(4, device="cuda", requires_grad=True)
+    loss = (q * p.grad).sum()
+    A.clip_grad_norm_([p], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
