@@ -45,3 +45,12 @@ def test_clip_tables_of_one_length():
                                           (at, at, *B.clip_tables([4], [0]))):
         with pytest.raises(ValueError, match="tensors"):
             B.rgnn_clip_grad_norm(grads, clipped, sizes, dtypes, 1.0, 1 << 30, 1 << 31)
+
+
+def test_stream_of_a_torch_without_its_internal_call(monkeypatch):
+    class Stream:
+        cuda_stream = 1234
+
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: Stream if device == 3 else None)
+    assert H._raw_stream(object())(3) == 1234
+    assert H._raw_stream(type("C", (), {"_cuda_getCurrentRawStream": staticmethod(lambda device: device + 1)}))(3) == 4
