@@ -331,18 +331,20 @@ Plan plan(const rgnn_norm_desc_t* d) {
 }
 
 template <int N> using Int = std::integral_constant<int, N>;
-template <typename F>
+// ALL16: every tensor is bf16
+template <bool ALL16, typename F>
 rgnn_status_t with_vectors(const rgnn_norm_desc_t* d, const Plan& p, F f) {
     auto count = [&](auto V, auto even) {
         return p.NV <= 1 ? f(V, Int<1>{}, even) : p.NV <= 2 ? f(V, Int<2>{}, even) : f(V, Int<4>{}, even);
     };
-    if (p.V == 8) return count(Int<8>{}, std::true_type{});
+    if constexpr (ALL16)
+        if (p.V == 8) return count(Int<8>{}, std::true_type{});
     return d->width % 4 == 0 ? count(Int<4>{}, std::true_type{}) : count(Int<4>{}, std::false_type{});
 }
 
 template <typename TX, typename TS, typename TO>
 rgnn_status_t launch_fwd(const rgnn_norm_desc_t* d, const Plan& p, const FwdArgs& a, hipStream_t st) {
-    return with_vectors(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
+    return with_vectors<sizeof(TX) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
         KernelTimer timer(st, "norm_fwd");
         norm_fwd_kernel<TX, TS, TO, V(), NV(), even()><<<p.blocks, kBlock, 0, st>>>(a);
         RGNN_CHECK_LAUNCH();
@@ -351,7 +353,7 @@ rgnn_status_t launch_fwd(const rgnn_norm_desc_t* d, const Plan& p, const FwdArgs
 }
 template <typename TX, typename TS, typename TO>
 rgnn_status_t launch_bwd(const rgnn_norm_desc_t* d, const Plan& p, const BwdArgs& a, hipStream_t st) {
-    return with_vectors(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
+    return with_vectors<sizeof(TX) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
         // at most 8 wavefronts' rows of 64 x 4 vectors of eight columns: 64 KB
         const size_t lds = sizeof(float) * (4 + (p.G <= 64 && a.part ? a.width : 0)) * (kBlock / 64);
         RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(norm_bwd_kernel<TX, TS, TO, V(), NV(), even()>), lds));
