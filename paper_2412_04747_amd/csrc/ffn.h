@@ -222,8 +222,15 @@ __device__ __forceinline__ void combine_block(const float* part, int splits, int
     store_cols<4>(out + i, sum);
 }
 
-// hidden values of a workgroup that forms the weights' gradients
-inline int ffn_grad_columns(const rgnn_ffn_desc_t* d) { return kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16); }
+constexpr int kBlockRows = 32 * kRowWaves;
+inline int ffn_chunks(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
+inline int ffn_row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 1) / kBlockRows); }
+
+// Workgroups that form the weights' gradients, by hidden values.
+inline int ffn_grad_groups(const rgnn_ffn_desc_t* d) {
+    const int columns = kRowWaves * (d->dtype == RGNN_BF16 && d->width < 128 ? 32 : 16);
+    return (d->hidden + columns - 1) / columns;
+}
 
 // Shares of the rows for them.  A share costs its sums of 3 d f fp32 written and read, 24 d f bytes at some 5 TB/s; a unit of 32 rows takes a
 // workgroup 0.016 d us (fp32: 0.04 d).  With n units the sum of both is least at sqrt(3333 n / f) shares (8333); `most` fill the GPU.

@@ -72,17 +72,14 @@ __global__ __launch_bounds__(256) void ffn_grad_reduce_kernel(FfnGradArgs k, int
     grad_reduce_block<T>(k, D, blockIdx.x, lds);
 }
 
-int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
-constexpr int kBlockRows = 32 * kRowWaves;
 constexpr int64_t kMostRows = 2000000000;      // HIP counts a launch's lanes, two per row, in 32 bits
 size_t packed_bytes(const rgnn_ffn_desc_t* d, bool backward) {
-    return align_up((size_t)chunks_of(d) * (backward ? 5 : 3) * (d->width / 16) * (d->dtype == RGNN_BF16 ? 1 : 3) * kFrag);
+    return align_up((size_t)ffn_chunks(d) * (backward ? 5 : 3) * (d->width / 16) * (d->dtype == RGNN_BF16 ? 1 : 3) * kFrag);
 }
-int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + ffn_grad_columns(d) - 1) / ffn_grad_columns(d); }
-int grad_splits(const rgnn_ffn_desc_t* d) { return ffn_grad_shares(d, std::max(4, 512 / grad_groups(d))); }
+int grad_splits(const rgnn_ffn_desc_t* d) { return ffn_grad_shares(d, std::max(4, 512 / ffn_grad_groups(d))); }
 size_t workspace_bytes(const rgnn_ffn_desc_t* d, bool backward) {
     if (ffn_few(d, backward)) return ffn_few_bytes(d, backward);
-    return packed_bytes(d, backward) + (backward ? align_up(sizeof(float) * (size_t)grad_splits(d) * 3 * d->width * chunks_of(d) * kHid) : 0);
+    return packed_bytes(d, backward) + (backward ? align_up(sizeof(float) * (size_t)grad_splits(d) * 3 * d->width * ffn_chunks(d) * kHid) : 0);
 }
 
 template <int D, int PL>
@@ -93,8 +90,6 @@ rgnn_status_t launch_pack(const FfnArgs& a, bool backward, unsigned char* to, hi
     RGNN_CHECK_LAUNCH();
     return RGNN_OK;
 }
-
-int row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 1) / kBlockRows); }
 
 rgnn_status_t forward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st) {
     unsigned char* const packed = static_cast<unsigned char*>(workspace);
@@ -132,8 +127,8 @@ rgnn_status_t grad_reduce(const rgnn_ffn_desc_t* d, const FfnGradArgs& k, hipStr
 rgnn_status_t backward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, int accumulate, void* workspace, hipStream_t st) {
     unsigned char* const packed = static_cast<unsigned char*>(workspace);
     const RowsArgs r{a, packed, dX, nullptr, 1, accumulate};
-    const FfnGradArgs k{a, reinterpret_cast<float*>(packed + packed_bytes(d, true)), grad_splits(d), grad_groups(d), dWg, dWu, dWd, accumulate};
-    const int rows = dX ? row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
+    const FfnGradArgs k{a, reinterpret_cast<float*>(packed + packed_bytes(d, true)), grad_splits(d), ffn_grad_groups(d), dWg, dWu, dWd, accumulate};
+    const int rows = dX ? ffn_row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
             if (rows) RGNN_TRY((launch_pack<D, PL>(a, true, packed, st)));
@@ -155,7 +150,6 @@ rgnn_status_t check_desc(const rgnn_ffn_desc_t* d) {
     RGNN_TRY(check_rows(d->rows));
     if (d->rows > kMostRows) RGNN_FAIL(RGNN_EUNSUPPORTED, "rows %lld not supported (up to %lld)", (long long)d->rows, (long long)kMostRows);
     RGNN_TRY(check_dtype(d->dtype));
-    
     if (d->width != 32 && d->width != 64 && d->width != 128) RGNN_FAIL(RGNN_EUNSUPPORTED, "width %d not supported (32/64/128)", d->width);
     if (d->hidden < 1) RGNN_FAIL(RGNN_EINVAL, "hidden %d is not positive", d->hidden);
     if (d->hidden > 16384) RGNN_FAIL(RGNN_EUNSUPPORTED, "hidden %d not supported (up to 16384)", d->hidden);
@@ -200,7 +194,7 @@ extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X
     const int32_t t = desc->dtype;
     RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t)},
                            {span(out, n, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, false)}}));
-    const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, nullptr};
+    const FfnArgs a{desc->rows, desc->hidden, ffn_chunks(desc), X, Wg, Wu, Wd, nullptr};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return ffn_few(desc, false) ? ffn_few_fwd(desc, a, out, workspace, st) : forward(desc, a, out, workspace, st);
 }
@@ -218,7 +212,7 @@ extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X
     RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t), span(dOut, n, t)},
                            {span(dX, n, t), span(dWg, w, t), span(dWu, w, t), span(dWd, w, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, true)}}));
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const FfnArgs a{desc->rows, desc->hidden, chunks_of(desc), X, Wg, Wu, Wd, dOut};
+    const FfnArgs a{desc->rows, desc->hidden, ffn_chunks(desc), X, Wg, Wu, Wd, dOut};
     const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
     if (desc->rows > 0 && ffn_few(desc, true)) return ffn_few_bwd(desc, a, dX, dWg, dWu, dWd, workspace, st);
     if (desc->rows == 0) dX = nullptr;

@@ -15,8 +15,6 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kBlockRows = 32 * kRowWaves;
-
 template <int D, int PL, bool BWD> constexpr int rows_lds() { return (BWD ? 5 : 3) * (D / 16) * PL * kFrag; }
 
 // 128 rows, a share of the chunks.
@@ -206,29 +204,26 @@ __global__ __launch_bounds__(256) void ffn_few_sum_kernel(RowsArgs r, FfnGradArg
     else grad_reduce_block<T>(k, D, b - row_blocks, lds);
 }
 
-int chunks_of(const rgnn_ffn_desc_t* d) { return (d->hidden + kHid - 1) / kHid; }
-int row_blocks(const rgnn_ffn_desc_t* d) { return (int)((d->rows + kBlockRows - 1) / kBlockRows); }
 // A chunk takes a workgroup 3 to 5 us, most of it latency, the launch that adds the shares 4: three chunks stay together, more are divided
 // as long as that puts a workgroup more on each compute unit, among 64 workgroups at most (a lane adds all shares of its values).
 int row_splits(const rgnn_ffn_desc_t* d) {
-    return chunks_of(d) <= 3 ? 1 : std::max(1, std::min({chunks_of(d), 64, 256 / std::max(row_blocks(d), 1)}));
+    return ffn_chunks(d) <= 3 ? 1 : std::max(1, std::min({ffn_chunks(d), 64, 256 / std::max(ffn_row_blocks(d), 1)}));
 }
 constexpr int kSingleRows = 4;
-int grad_groups(const rgnn_ffn_desc_t* d) { return (d->hidden + ffn_grad_columns(d) - 1) / ffn_grad_columns(d); }
 // (one or two units of 32 rows need no division)
-int grad_splits(const rgnn_ffn_desc_t* d) { return d->rows <= 2 * UNIT ? 1 : ffn_grad_shares(d, std::max(1, 256 / grad_groups(d))); }
+int few_grad_splits(const rgnn_ffn_desc_t* d) { return d->rows <= 2 * UNIT ? 1 : ffn_grad_shares(d, std::max(1, 256 / ffn_grad_groups(d))); }
 size_t share_bytes(const rgnn_ffn_desc_t* d) {
     const int s = row_splits(d);
     return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
 }
 size_t grad_bytes(const rgnn_ffn_desc_t* d) {
-    const int s = grad_splits(d);
-    return s > 1 ? align_up(sizeof(float) * (size_t)s * 3 * d->width * chunks_of(d) * kHid) : 0;
+    const int s = few_grad_splits(d);
+    return s > 1 ? align_up(sizeof(float) * (size_t)s * 3 * d->width * ffn_chunks(d) * kHid) : 0;
 }
 
 rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs& k, hipStream_t st) {
     const unsigned rows = r.splits > 1 ? (unsigned)((d->rows * d->width / 4 + 255) / 256) : 0;
-    const unsigned grads = k.splits > 1 ? (unsigned)((int64_t)3 * d->width * chunks_of(d) * kHid / 64) : 0;
+    const unsigned grads = k.splits > 1 ? (unsigned)((int64_t)3 * d->width * ffn_chunks(d) * kHid / 64) : 0;
     if (rows + grads == 0) return RGNN_OK;
     KernelTimer timer(st, "ffn_few.sum");
     if (d->dtype == RGNN_BF16) ffn_few_sum_kernel<bf16_t><<<rows + grads, 256, 0, st>>>(r, k, d->width, (int)rows);
@@ -270,7 +265,7 @@ rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out,
             auto* const kernel = ffn_few_fwd_kernel<D, PL, ACT>;
             RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
             KernelTimer timer(st, "ffn_few_fwd");
-            kernel<<<dim3(row_blocks(d), r.splits), 64 * kRowWaves, lds, st>>>(r);
+            kernel<<<dim3(ffn_row_blocks(d), r.splits), 64 * kRowWaves, lds, st>>>(r);
             RGNN_CHECK_LAUNCH();
             return RGNN_OK;
         });
@@ -284,8 +279,8 @@ rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out,
 rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st) {
     const int accumulate = (d->flags & RGNN_FLAG_ACCUMULATE) != 0;
     RowsArgs r{a, nullptr, dX, static_cast<float*>(workspace), row_splits(d), accumulate};
-    FfnGradArgs k{a, reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d)), grad_splits(d), grad_groups(d), dWg, dWu, dWd, accumulate};
-    const int rows = dX ? row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
+    FfnGradArgs k{a, reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d)), few_grad_splits(d), ffn_grad_groups(d), dWg, dWu, dWd, accumulate};
+    const int rows = dX ? ffn_row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
     if (rows + grads == 0) return RGNN_OK;
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
