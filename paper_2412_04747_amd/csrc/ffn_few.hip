@@ -204,16 +204,22 @@ __global__ __launch_bounds__(256) void ffn_few_sum_kernel(RowsArgs r, FfnGradArg
     else grad_reduce_block<T>(k, D, b - row_blocks, lds);
 }
 
-// A chunk takes a workgroup 3 to 5 us, most of it latency, the launch that adds the shares 4: three chunks stay together, more are divided
-// as long as that puts a workgroup more on each compute unit, among 64 workgroups at most (a lane adds all shares of its values).
-int row_splits(const rgnn_ffn_desc_t* d) {
-    return ffn_chunks(d) <= 3 ? 1 : std::max(1, std::min({ffn_chunks(d), 64, 256 / std::max(ffn_row_blocks(d), 1)}));
-}
-constexpr int kSingleRows = 4;
 // (one or two units of 32 rows need no division)
 int few_grad_splits(const rgnn_ffn_desc_t* d) { return d->rows <= 2 * UNIT ? 1 : ffn_grad_shares(d, std::max(1, 256 / ffn_grad_groups(d))); }
-size_t share_bytes(const rgnn_ffn_desc_t* d) {
-    const int s = row_splits(d);
+// Chunks that stay together; more are divided as long as that puts a workgroup more on each compute unit, among 64 workgroups at most (a lane adds
+// all shares of its values).  Forward, that is a second launch, and for bf16, whose chunks are short, three are done sooner; backward the sums'
+// launch is there anyway with more than 64 rows, and otherwise costs less than a chunk but for bf16 up to width 64.  In us, undivided / divided:
+//   forward   d 64, bf16: 2 chunks, 256 rows 5.6 / 6.5, 3 chunks 7.0 / 7.0; fp32: 2 chunks 9.5 / 9.2 (a call, with its launches, 9.3 / 9.6), 3 chunks 12.0 / 9.5
+//   backward  2 chunks, 256 rows, d 32, bf16: 9.2 / 7.4; d 64, fp32: 18.7 / 13.4; d 128, bf16: 20.0 / 14.3
+//             60 rows, 2 chunks, d 64, bf16: 9.0 / 10.9; 3 chunks, d 64, bf16: 11.0 / 11.9, fp32: 17.9 / 11.7; d 128, bf16: 18.7 / 13.2
+int row_splits(const rgnn_ffn_desc_t* d, bool backward) {
+    const bool bf16 = d->dtype == RGNN_BF16;
+    const int together = backward ? bf16 && d->width < 128 && few_grad_splits(d) == 1 ? 3 : 1 : bf16 ? 3 : 2;
+    return ffn_chunks(d) <= together ? 1 : std::max(1, std::min({ffn_chunks(d), 64, 256 / std::max(ffn_row_blocks(d), 1)}));
+}
+constexpr int kSingleRows = 4;
+size_t share_bytes(const rgnn_ffn_desc_t* d, bool backward) {
+    const int s = row_splits(d, backward);
     return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
 }
 size_t grad_bytes(const rgnn_ffn_desc_t* d) {
@@ -247,10 +253,10 @@ bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
     if (f32) return d->rows <= (backward || d->width == 128 ? 8192 : 2560);
     return d->rows <= (backward ? 2560 : 1024);
 }
-size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d) + (backward ? grad_bytes(d) : 0)); }
+size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d, backward) + (backward ? grad_bytes(d) : 0)); }
 
 rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st) {
-    const RowsArgs r{a, nullptr, out, static_cast<float*>(workspace), row_splits(d), 0};
+    const RowsArgs r{a, nullptr, out, static_cast<float*>(workspace), row_splits(d, false), 0};
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
             if (d->rows <= kSingleRows) {
@@ -278,8 +284,8 @@ rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out,
 
 rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st) {
     const int accumulate = (d->flags & RGNN_FLAG_ACCUMULATE) != 0;
-    RowsArgs r{a, nullptr, dX, static_cast<float*>(workspace), row_splits(d), accumulate};
-    FfnGradArgs k{a, reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d)), few_grad_splits(d), ffn_grad_groups(d), dWg, dWu, dWd, accumulate};
+    RowsArgs r{a, nullptr, dX, static_cast<float*>(workspace), row_splits(d, true), accumulate};
+    FfnGradArgs k{a, reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d, true)), few_grad_splits(d), ffn_grad_groups(d), dWg, dWu, dWd, accumulate};
     const int rows = dX ? ffn_row_blocks(d) : 0, grads = dWg ? k.splits * k.groups : 0;
     if (rows + grads == 0) return RGNN_OK;
     auto run = [&]() -> rgnn_status_t {
