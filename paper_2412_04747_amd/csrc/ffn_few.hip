@@ -217,7 +217,11 @@ int row_splits(const rgnn_ffn_desc_t* d, bool backward) {
     const int together = backward ? bf16 && d->width < 128 && few_grad_splits(d) == 1 ? 3 : 1 : bf16 ? 3 : 2;
     return ffn_chunks(d) <= together ? 1 : std::max(1, std::min({ffn_chunks(d), 64, 256 / std::max(ffn_row_blocks(d), 1)}));
 }
+// Rows up to which the forward takes no matrix instructions.  Theirs, of bf16, are as soon done with two rows.  In us, with them / without:
+//   1 row          d 64, f 256, bf16: 5.5 / 4.7, fp32: 6.9 / 4.7; d 128, f 341, bf16: 7.3 / 6.2, fp32: 10.2 / 5.8; f 2048, bf16: 10.4 / 9.2, fp32: 13.8 / 9.4
+//   2, 3, 4 rows   d 64, f 256, bf16: 5.5 / 5.9, fp32: 7.0 / 5.8; d 128, f 341, bf16: 7.3 / 8.7, fp32: 10.4 / 8.8; f 2048, bf16: 10.4 / 11.9, fp32: 13.5 / 12.1
 constexpr int kSingleRows = 4;
+bool single(const rgnn_ffn_desc_t* d) { return d->rows <= (d->dtype == RGNN_F32 ? kSingleRows : 1); }
 size_t share_bytes(const rgnn_ffn_desc_t* d, bool backward) {
     const int s = row_splits(d, backward);
     return s > 1 ? align_up(sizeof(float) * (size_t)s * d->rows * d->width) : 0;
@@ -259,11 +263,11 @@ rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out,
     const RowsArgs r{a, nullptr, out, static_cast<float*>(workspace), row_splits(d, false), 0};
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
-            if (d->rows <= kSingleRows) {
+            if (single(d)) {
                 using T = typename std::conditional<PL == 1, bf16_t, float>::type;
                 KernelTimer timer(st, "ffn_single_fwd");
-                if (d->rows == 1) ffn_single_fwd_kernel<D, T, ACT, 1><<<r.splits, 256, 0, st>>>(r);
-                else ffn_single_fwd_kernel<D, T, ACT, kSingleRows><<<r.splits, 256, 0, st>>>(r);
+                if (PL == 1 || d->rows == 1) ffn_single_fwd_kernel<D, T, ACT, 1><<<r.splits, 256, 0, st>>>(r);
+                else if constexpr (PL == 3) ffn_single_fwd_kernel<D, T, ACT, kSingleRows><<<r.splits, 256, 0, st>>>(r);
                 RGNN_CHECK_LAUNCH();
                 return RGNN_OK;
             }
