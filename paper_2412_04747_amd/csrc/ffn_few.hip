@@ -4,7 +4,7 @@
 // the backward's two passes share a launch, some of its workgroups forming dX and the others the weights' gradients; and what several
 // workgroups add up is summed by one launch for both.  A call is two launches, or one where nothing is divided.  1000 rows, d 64, f 256, bf16, backward:
 // 13.4 us, 32 with a launch that lays out the weights and one for each pass and sum.
-// Every 128 rows read and split all weights again, which is worth it up to some number of rows (ffn_few).
+// ffn_few says which calls are such.
 #include <math.h>
 
 #include "rgnn_internal.h"
@@ -212,10 +212,12 @@ int few_grad_splits(const rgnn_ffn_desc_t* d) { return d->rows <= 2 * UNIT ? 1 :
 //   forward   d 64, bf16: 2 chunks, 256 rows 5.6 / 6.5, 3 chunks 7.0 / 7.0; fp32: 2 chunks 9.5 / 9.2 (a call, with its launches, 9.3 / 9.6), 3 chunks 12.0 / 9.5
 //   backward  2 chunks, 256 rows, d 32, bf16: 9.2 / 7.4; d 64, fp32: 18.7 / 13.4; d 128, bf16: 20.0 / 14.3
 //             60 rows, 2 chunks, d 64, bf16: 9.0 / 10.9; 3 chunks, d 64, bf16: 11.0 / 11.9, fp32: 17.9 / 11.7; d 128, bf16: 18.7 / 13.2
-int row_splits(const rgnn_ffn_desc_t* d, bool backward) {
+int kept_together(const rgnn_ffn_desc_t* d, bool backward) {
     const bool bf16 = d->dtype == RGNN_BF16;
-    const int together = backward ? bf16 && d->width < 128 && few_grad_splits(d) == 1 ? 3 : 1 : bf16 ? 3 : 2;
-    return ffn_chunks(d) <= together ? 1 : std::max(1, std::min({ffn_chunks(d), 64, 256 / std::max(ffn_row_blocks(d), 1)}));
+    return backward ? bf16 && d->width < 128 && few_grad_splits(d) == 1 ? 3 : 1 : bf16 ? 3 : 2;
+}
+int row_splits(const rgnn_ffn_desc_t* d, bool backward) {
+    return ffn_chunks(d) <= kept_together(d, backward) ? 1 : std::max(1, std::min({ffn_chunks(d), 64, 256 / std::max(ffn_row_blocks(d), 1)}));
 }
 // Rows up to which the forward takes no matrix instructions.  Theirs, of bf16, are as soon done with two rows.  In us, with them / without:
 //   1 row          d 64, f 256, bf16: 5.5 / 4.7, fp32: 6.9 / 4.7; d 128, f 341, bf16: 7.3 / 6.2, fp32: 10.2 / 5.8; f 2048, bf16: 10.4 / 9.2, fp32: 13.8 / 9.4
@@ -244,18 +246,34 @@ rgnn_status_t sum(const rgnn_ffn_desc_t* d, const RowsArgs& r, const FfnGradArgs
 
 }  // namespace
 
-// Up to which number of rows this is faster than laying out the weights first, in us here / there:
-//   forward   d 32, f 64, bf16: 32000 rows 5.1 / 5.6; fp32: 32000 7.9 / 8.8
-//             d 64, f 256, bf16: 300 6.8 / 7.1, 2000 8.3 / 7.3; fp32: 2000 11.0 / 12.2, 4000 13.8 / 12.3
-//             d 128, f 341, bf16: 300 10.0 / 11.5, 2000 14.2 / 11.8; fp32: 8000 29.5 / 31.3, 12000 41.5 / 31.8
-//   backward  d 32, f 64, bf16: 12000 11.6 / 12.7, 24000 16.0 / 15.2; fp32: 32000 20.1 / 26.9
-//             d 64, f 256, bf16: 2000 16.7 / 18.3, 4000 24.0 / 19.6; fp32: 8000 39.8 / 42.6, 12000 52.7 / 43.4
-//             d 128, f 341, bf16: 2000 30.8 / 31.3, 4000 35.8 / 33.5; fp32: 8000 81.3 / 87.6, 12000 121 / 109
+// Whether this is faster than laying out the weights first.  Every 128 rows read and split all weights again, and a workgroup waits for each of its chunks;
+// that is for few rows, or few chunks.
+// Forward, chunks that stay together: one launch for two, with as many chunks as take less than the second launch.  Divided ones: the shares to write
+// and add grow with the rows, what the laid-out pass takes longer at the least with the chunks and the width: up to sqrt(60 d f) rows (fp32 400), f up to 2048.
+// Backward, always a second launch: by rows, types and width, and of width 32, whose chunks are the shortest, fewer rows where there are several of them.
+// Microseconds of a call, hidden values f and rows, here / laid out first:
+//   forward  d 32, bf16: f 64, 1000: 5.0 / 7.5; 32000: 5.3 / 7.7; f 128, 512: 7.2 / 7.5; 5000: 7.3 / 7.5; f 512, 512: 7.8 / 8.3; 2500: 9.5 / 7.8; 32000: 20.6 / 13.2; f 2048, 1500: 12.8 / 13.4; 5000: 19.4 / 13.5; 32000: 74.0 / 37.4
+//   forward  d 32, fp32: f 96, 1000: 8.4 / 8.0; 16000: 11.9 / 8.6; f 512, 1500: 10.2 / 11.4; 5000: 13.7 / 11.7; f 2048, 3500: 23.7 / 26.5; 32000: 121 / 76.7
+//   forward  d 64, bf16: f 64, 8000: 6.0 / 7.8; f 256, 512: 7.5 / 7.7; 2500: 9.5 / 7.7; f 2048, 2500: 18.3 / 19.3; 8000: 30.8 / 19.9
+//   forward  d 64, fp32: f 64, 1000: 9.6 / 9.0; f 256, 2500: 12.3 / 12.3; 5000: 16.6 / 12.5; f 2048, 5000: 40.7 / 47.5
+//   forward  d 128, bf16: f 32, 1000: 6.5 / 7.8; f 64, 1000: 8.4 / 7.8; f 512, 1500: 14.9 / 15.0; 5000: 20.7 / 15.1
+//   forward  d 128, fp32: f 32, 1000: 11.5 / 13.3; f 64, 1000: 15.9 / 12.7; f 512, 5000: 31.2 / 38.3; 12000: 50.4 / 39.8
+//   backward d 32, bf16: f 32, 16000: 12.6 / 13.6; f 128, 5000: 13.0 / 13.7; 16000: 19.7 / 17.1; f 2048, 8000: 50.3 / 64.2; 16000: 83.1 / 67.6
+//   backward d 32, fp32: f 256, 32000: 44.3 / 46.4; f 2048, 12000: 131 / 138; 32000: 289 / 270
+//   backward d 64, bf16: f 128, 2500: 14.4 / 15.7; 8000: 25.9 / 19.2; f 2048, 5000: 75.8 / 80.1; 8000: 104 / 83.0
+//   backward d 64, fp32: f 256, 8000: 39.2 / 41.6; 12000: 51.8 / 42.8
+//   backward d 128, bf16: f 256, 2500: 29.7 / 30.5; 5000: 35.4 / 31.6
+//   backward d 128, fp32: f 256, 5000: 60.3 / 67.6; 12000: 93.5 / 77.2
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
     const bool f32 = d->dtype == RGNN_F32;
-    if (d->width == 32) return d->rows <= (f32 || !backward ? 32768 : 16384);
-    if (f32) return d->rows <= (backward || d->width == 128 ? 8192 : 2560);
-    return d->rows <= (backward ? 2560 : 1024);
+    const int chunks = ffn_chunks(d);
+    if (backward) {
+        if (d->width == 32) return d->rows <= (f32 ? chunks <= 8 ? 32768 : 12288 : chunks == 1 ? 32768 : 8192);
+        return d->rows <= (f32 ? d->width == 64 ? 8192 : 6144 : d->width == 64 ? 3584 : 3072);
+    }
+    if (single(d)) return true;
+    if (chunks <= kept_together(d, false)) return d->rows <= 32768 && (chunks == 1 || chunks * d->width * (f32 ? 3 : 1) <= 192);
+    return d->rows <= 8192 && d->rows * d->rows <= (int64_t)(f32 ? 400 : 60) * d->width * std::min(d->hidden, 2048);
 }
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward) { return std::max<size_t>(256, share_bytes(d, backward) + (backward ? grad_bytes(d) : 0)); }
 
