@@ -7,10 +7,11 @@
 // order in which the instructions read them (as planes, padded with zeros to whole chunks), come through the LDS for the four
 // wavefronts of a workgroup: bf16 in two places that take turns, fp32 in one whose two halves do.  Nothing of the hidden width is written.
 //
-// Matrix instructions bound it, 6 N d f operations forward and 16 N d f backward (22 as the hidden values are formed twice), sixfold for fp32;
-// in bf16 up to width 64 the vector instructions, an exponential and a reciprocal per hidden value.  Against 1160 TFLOP/s of a large bf16 product:
-//   forward   2M rows, d 128, f 512, bf16: 1015 us, 775 TFLOP/s (one plane more of h in the last product: 1030 of what is done); 1M rows, d 64, f 256, bf16: 155 us, 630; fp32: 498 us, 1180 of plane products
-//   backward  200017 rows, d 128, f 341, bf16: 311 us, 620 of the 22 (900 of the 32 that the second planes make of them); 1M rows, d 64, f 256, fp32: 1860 us, 1160 of plane products
+// Matrix instructions bound it, 6 N d f operations forward and 16 N d f backward (22 as the hidden values are formed twice), sixfold for fp32; bf16's second
+// plane of h, dg and du makes 8 of the 6 and 32 of the 22.  In bf16 up to width 64 the vector instructions are as long, an exponential and a reciprocal per
+// hidden value.  Against 1160 TFLOP/s of a large bf16 product, in brackets what the matrix instructions do:
+//   forward   2M rows, d 128, f 512, bf16: 1007 us, 781 TFLOP/s (1040); 1M rows, d 64, f 256, bf16: 174 us, 565 (753); fp32: 520 us, 189 (1134)
+//   backward  200017 rows, d 128, f 341, bf16: 311 us, 449 (900); 1M rows, d 64, f 256, bf16: 669 us, 392 (783); fp32: 1901 us, 138 (1138)
 #include <math.h>
 
 #include "rgnn_internal.h"

@@ -85,10 +85,16 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
         for (int k = 0; k < (BWD ? 3 : 2); ++k) operand(w + (k * S + s) * PL * kFrag, o.f[k]);
         return o;
     };
-    auto read_second = [&](const unsigned char* w, int q) {           // q = TILES s + t
+    // Steps of the second products: tile and half of the chunk's hidden values.  One plane: the first halves of all tiles while the second's values are
+    // split; three: a tile's halves after each other, whose products are summed on their own and then added, one rounding at the result's magnitude per
+    // 32 hidden values instead of twelve (1M rows, d 64, f 256, error of dX against 64 bits 3.9e-7 before; f 16384 2.8e-6).
+    constexpr bool OWN = PL == 3;
+    auto tile = [](int q) { return OWN ? q / 2 : q % TILES; };
+    auto part = [](int q) { return OWN ? q % 2 : q / TILES; };
+    auto read_second = [&](const unsigned char* w, int q) {
         SecondOps o;
 #pragma unroll
-        for (int k = 0; k < (BWD ? 2 : 1); ++k) operand(w + (k * S + 2 * (q % TILES) + q / TILES) * PL * kFrag, o.f[k]);
+        for (int k = 0; k < (BWD ? 2 : 1); ++k) operand(w + (k * S + 2 * tile(q) + part(q)) * PL * kFrag, o.f[k]);
         return o;
     };
     // the s-th sixteen columns' share of the chunk's hidden values
@@ -105,17 +111,29 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
             planes8<HP>(*reinterpret_cast<const float(*)[8]>(v + 8 * s), p[s]);
             if constexpr (BWD) planes8<HP>(*reinterpret_cast<const float(*)[8]>(v2 + 8 * s), p2[s]);
         };
+        // (forward, the previous tile's is added while this one's instructions run; the backward has no registers left for a second)
+        constexpr int OWNS = BWD ? 1 : 2;
+        v16f own[OWNS];
+        auto add = [&](int t) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[t][i] += own[t % OWNS][i];
+        };
         round(0);
 #pragma unroll
         for (int q = 0; q < S; ++q) {
             if (q + DEPTH - 1 < S) o[(q + DEPTH - 1) % DEPTH] = read_second(second(c), q + DEPTH - 1);
             fence();
-            const int s = q / TILES, t = q % TILES;
-            mul_add(o[q % DEPTH].f[0], p[s], y[t]);
-            if constexpr (BWD) mul_add(o[q % DEPTH].f[1], p2[s], y[t]);
+            const int s = part(q), t = tile(q);
+            if (OWN && s == 0) clear(own[t % OWNS]);
+            v16f& to = OWN ? own[t % OWNS] : y[t];
+            mul_add(o[q % DEPTH].f[0], p[s], to);
+            if constexpr (BWD) mul_add(o[q % DEPTH].f[1], p2[s], to);
             if (q == 0) round(1);
+            if (OWN && OWNS == 1 && s == 1) add(t);
+            if (OWN && OWNS == 2 && s == 0 && t > 0) add(t - 1);
             fence();
         }
+        if (OWN && OWNS == 2) add(TILES - 1);
     };
     auto read_early = [&](int c, SecondOps (&o)[DEPTH]) {
 #pragma unroll
