@@ -260,16 +260,17 @@ def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
     if not given:
         return torch.zeros(())
     for g in given:
-        if g.layout != torch.strided or g.dtype not in (torch.float32, torch.bfloat16) or not g.is_cuda or g.device != given[0].device:
+        if g.layout != torch.strided or g.dtype not in _CODES or not g.is_cuda or g.device != given[0].device:
             raise TypeError("clip_grad_norm_ takes dense fp32 or bf16 gradients on one GPU")
+    # (strided ones reach the library as copies, whose own memory it compares)
+    strided = [g for g in given if not _dense(g)]
+    for g in strided:
         if not _apart(g):
             raise RuntimeError(f"clip_grad_norm_: elements of a gradient share memory (shape {tuple(g.shape)}, strides {g.stride()})")
+    if len({g.data_ptr() for g in strided if g.numel()}) < sum(g.numel() > 0 for g in strided):
+        raise RuntimeError("clip_grad_norm_: two gradients share memory")
     with torch.cuda.device(given[0].device):
-        # (strided ones reach the library as copies, whose own memory it compares)
-        strided = [g.data_ptr() for g in given if g.numel() and not _dense(g)]
-        if len(set(strided)) < len(strided):
-            raise RuntimeError("clip_grad_norm_: two gradients share memory")
-        grads = [g if _dense(g) else g.contiguous() for g in given]
+        grads = [g if _dense(g) else g.contiguous() for g in given] if strided else given
         sizes = [g.numel() for g in grads]
         norm = torch.empty((), device=given[0].device)
         dtypes, ws = [_code(g.dtype) for g in grads], _buf(B.rgnn_clip_workspace_bytes(sizes))
@@ -279,9 +280,10 @@ def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
                 raise RuntimeError(f"the norm of the gradients is {norm.item()}, so that they cannot be clipped")
         B.rgnn_clip_grad_norm(grads, grads, sizes, dtypes, float(max_norm), norm, ws, _stream())
         torch.autograd.graph.increment_version([g for g, c in zip(given, grads) if c is g])
-        for g, c in zip(given, grads):
-            if c is not g:
-                g.copy_(c)
+        if strided:
+            for g, c in zip(given, grads):
+                if c is not g:
+                    g.copy_(c)
     return norm
 
 
