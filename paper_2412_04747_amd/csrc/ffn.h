@@ -75,7 +75,8 @@ __device__ __forceinline__ void clear(Acc& c) {
 }
 
 // act(g) and its derivative.  silu: g s and s (1 + g (1 - s)), s = 1 / (1 + exp(-g)) by the base-2 exponential and reciprocal
-// instructions, each right to one unit in the last place.
+// instructions, each right to one unit in the last place.  The exponent, g times a rounded constant, is off by up to |g| units in all, which is what g's
+// own rounding moves the exponential by: far out on the negative side s has |g| units less, of a value below exp(-|g|).
 template <int ACT>
 __device__ __forceinline__ float act(float g) {
     if (ACT == RGNN_ACT_RELU) return g <= 0.f ? 0.f : g;       // (NaN stays)

@@ -58,7 +58,8 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, false>::per_simd)) 
 }
 
 // The backward's two passes in one launch: workgroups [0, row_blocks) take the rows, the others the weights' gradients.  Neither waits for
-// the other's last workgroups (two launches / one: 16500 rows, d 64, f 256, bf16, 40.8 / 31.9 us; 64000 rows 51.0 / 47.5; 500000 rows, fp32, 921 / 908).
+// the other's last workgroups (either by itself, in sum / both in one: 14000 rows, d 64, f 256, bf16, 37.3 / 26.6 us; 200017 rows, d 128, f 341, 322 / 300;
+// 1M rows, d 64, f 256, 605 / 592; fp32, 1832 / 1858).
 template <int D, int PL, int ACT>
 __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, true>::per_simd)) void ffn_bwd_kernel(RowsArgs r, FfnGradArgs k, int row_blocks) {
     extern __shared__ unsigned char lds[];
@@ -107,7 +108,7 @@ rgnn_status_t forward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, voi
             return RGNN_OK;
         };
         // While there is less than a workgroup of 128 rows for every second compute unit, the wavefronts of a workgroup divide the chunks
-        // instead (8000 rows, undivided / divided: d 64, f 256, bf16 9.7 / 7.4 us, fp32 20.2 / 12.7; d 128, f 341, 15.0 / 12.0 and 42.4 / 30.8).
+        // instead (8000 rows, undivided / divided: d 64, f 256, bf16 10.8 / 8.1 us, fp32 20.7 / 13.0; d 128, f 341, bf16 16.7 / 13.4, 9000 rows, fp32, 45.2 / 32.2).
         constexpr int most = D == 128 ? 2 : 4;           // (four groups' places at width 128 exceed the LDS)
         if (most == 4 && d->rows <= 256 * 32 && a.chunks >= 4) return launch(std::integral_constant<int, most>{});
         if (d->rows <= 256 * 64 && a.chunks >= 2) return launch(std::integral_constant<int, 2>{});

@@ -3,7 +3,7 @@
 // The weights are read as they are given and put into the LDS as operands by the workgroups that use them, so that no launch lays them out first;
 // the backward's two passes share a launch, some of its workgroups forming dX and the others the weights' gradients; and what several
 // workgroups add up is summed by one launch for both.  A call is two launches, or one where nothing is divided.  1000 rows, d 64, f 256, bf16, backward:
-// 13.4 us, 32 with a launch that lays out the weights and one for each pass and sum.
+// 13.5 us, 19 over weights that a launch laid out.
 // ffn_few says which calls are such.
 #include <math.h>
 
@@ -109,9 +109,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_fwd_kernel(RowsArgs
     few_rows_block<D, PL, ACT, false>(r, blockIdx.x, blockIdx.y, lds);
 }
 
-// A few rows by themselves, forward: no matrix instructions, whose 32 rows would be padding.  A workgroup takes 32 hidden values at a time: its lanes read 32
+// One row, or up to four in fp32, forward: no matrix instructions, whose 32 rows would be padding.  A workgroup takes 32 hidden values at a time: its lanes read 32
 // consecutive ones of a row of Wg and Wu, eight ranges of the columns beside each other, and then rows of Wd, every weight once and coalesced; sums meet in the
-// LDS.  (One row, d 128, f 512, fp32: 8.6 us in the kernel above, and the sum 4; with the call, 11.0 us for 7.8 here.)
+// LDS.  (One row, d 128, f 512, fp32: 10.4 us in the kernel above, 6.1 here.)
 template <int D, typename T, int ACT, int R>
 __global__ __launch_bounds__(256) void ffn_single_fwd_kernel(RowsArgs r) {
     constexpr int KG = 8, K = D / KG, HG = 256 / D, H = kHid / HG;

@@ -7,8 +7,8 @@
 // wavefronts of the workgroup, one unit ahead.
 // g, u and dh are formed a second time (the pass of the rows has them with the hidden values along): three products more of eleven, against
 // three tensors of the hidden width written and read, six times the bytes of the row tensors at f = 2 d.
-// MT = 32 for bf16 up to width 64; 16 otherwise, so that two wavefronts share a SIMD (fp32, 1M rows, d 64, f 256, this pass alone: 1086 us with 32, 889
-// with 16; bf16, 200017 rows, d 128, f 341: over 600 and 152), or, for fp32 at width 128, that the registers suffice at all.
+// MT = 32 for bf16 up to width 64 (1M rows, d 64, f 256, this pass alone: 320 us, 344 with 16); 16 otherwise, where 32 exceed the registers that leave two
+// wavefronts per SIMD (fp32, the same size: 977 us, 1965 with 32; bf16, 200017 rows, d 128, f 341: 178 and 1254).
 // Rows are divided among workgroups in interleaved shares, which another launch adds in order.
 #pragma once
 #include "ffn.h"

@@ -32,8 +32,8 @@ template <int D, int PL, bool BWD> struct Weights {
 
 // Wavefronts that share a SIMD, and whether the products of chunk c + 1 are issued between the activations of chunk c (the matrix unit and
 // the vector unit then work at the same time within a wavefront, which takes the registers of a second set of hidden values).  A second wavefront per
-// SIMD is worth more where the registers allow only one of both: backward, 1M rows, d 64, f 256, fp32, this pass 965 us with one wavefront and the
-// second set, 830 with two and without.
+// SIMD is worth more where the registers allow only one of both: backward, 1M rows, d 64, f 256, fp32, this pass 950 us with one wavefront and the
+// second set, 855 with two and without.
 template <int D, int PL, bool BWD> struct RowsCut {
     static constexpr int per_simd = D == 128 && PL == 3 && BWD ? 1 : 2;
     static constexpr bool ahead = !((BWD && (D == 128 || PL == 3)) || (D == 128 && PL == 3));
@@ -74,8 +74,8 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
     for (int t = 0; t < TILES; ++t) clear(y[t]);
 
     // Operands are read from the LDS a step before they are multiplied.  The compiler would move the reads to their use and wait there; the
-    // backward, whose registers are full, is left to it (2M rows, d 128, f 512, bf16, forward: 935 us without the fences, 913 with;
-    // 200017 rows, f 341, this pass of the backward: 119 and 134).
+    // backward, whose registers are full, is left to it (2M rows, d 128, f 512, bf16, forward: 1061 us without the fences, 1050 with;
+    // 200017 rows, f 341, backward: 300 and 306).
     auto fence = [] { if constexpr (!BWD) __builtin_amdgcn_sched_barrier(0); };
     struct FirstOps { bf16x8 f[BWD ? 3 : 2][PL]; };
     struct SecondOps { bf16x8 f[BWD ? 2 : 1][PL]; };

@@ -25,7 +25,9 @@ namespace rgnn {
 namespace {
 
 constexpr int kBlock = 512;              // threads of a workgroup
-constexpr int kMaxBlocks = 1024;         // four per compute unit hold all 32 wavefronts of its SIMDs
+// Four workgroups per compute unit hold all 32 wavefronts of its SIMDs, where the registers allow it: the forward of up to 16 columns per lane.  The backward
+// takes 88 to 98 registers with two vectors of four (two resident), 76 with one of eight (three): its workgroups then come in uneven turns.
+constexpr int kMaxBlocks = 1024;
 constexpr int kMaxWidth = 8192;
 
 // Columns c .. c + V - 1 of a row, those before `width`.  EVEN: the width is a multiple of V and rows start at multiples of 16 bytes (8 for
