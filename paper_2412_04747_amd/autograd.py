@@ -7,8 +7,8 @@ tape.  The layers are fp32 (the training protocol of the thesis' evaluation sect
 training of a two-layer model with a negative-log-likelihood loss).
 
 `residual_norm` and `gated_ffn` (`ResidualNorm`, `GatedFfn`) are what stands between the layers of a residual
-model; they take fp32 or bf16 rows and need no graph.  `clip_grad_norm_` bounds the global norm of a model's
-gradients before the optimiser's step.
+model; they take fp32 or bf16 rows and need no graph (the layers here are fp32 only; the C calls also take bf16 rows).
+`clip_grad_norm_` bounds the global norm of a model's gradients before the optimiser's step.
 
 The workspace of a (layer kind, width, options) combination is allocated once per graph, kept on the
 `Graph` object and dropped by `Graph.close()`; every call of that combination on the graph reuses it,
@@ -253,7 +253,7 @@ def _apart(t):
 def clip_grad_norm_(parameters, max_norm, error_if_nonfinite=False):
     """Scales the gradients of `parameters` in place by min(1, max_norm / (norm + 1e-6)), norm the 2-norm of all of them together, and
     returns that norm (0-dim fp32 tensor on the GPU; nothing waits for it unless error_if_nonfinite).  Gradients are fp32 or bf16, on one
-    GPU; two that share memory are refused (of strided ones, that begin at the same place)."""
+    GPU; contiguous ones that share memory are refused, and strided ones that begin at the same place.  Without any, a zero on the CPU."""
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
     given = [p.grad for p in parameters if p.grad is not None]

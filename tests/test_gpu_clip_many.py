@@ -31,7 +31,12 @@ def test_against_the_definition(count):
     _check([whole], [torch.cat(grads)], L.norm, 0.25 * want)
     assert (L.ws[n:] == 0xA5).all()
     first = float(L.norm)
+    alone = torch.zeros((), device="cuda")               # the norm without clipping
+    B.rgnn_clip_grad_norm([whole], None, [whole.numel()], [B.RGNN_F32], 0.0, alone, L.ws)
+    assert abs(float(alone) - want) <= want * 1.01 * 2.0 ** -24
     again = _tensors(count, count)
+    B.rgnn_clip_grad_norm(again, None, L.sizes, L.dtypes, 0.0, alone, L.ws)
+    assert float(alone) == first
     L.clip(again, math.inf)                              # the same bits again, and nothing scaled
     assert float(L.norm) == first and torch.equal(torch.cat(again), whole)
 
