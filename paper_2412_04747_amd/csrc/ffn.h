@@ -20,7 +20,7 @@ typedef unsigned rgnn_v2u __attribute__((ext_vector_type(2)));
 constexpr int kHid = 32;                 // hidden values of a chunk
 
 // Planes in which act(g) u, dg and du enter the next product.  bf16: two, 16 bits.  One would round them to bfloat16 there, an error of 2.3e-3
-// in the result where its own rounding makes 1.7e-3; with two the result is the rounded one but for a value in a hundred next to a border.
+// in the result where its own rounding makes 1.7e-3; with two the result is the rounded one but for a value in a thousand next to a border.
 constexpr int hidden_planes(int planes) { return planes == 1 ? 2 : planes; }
 
 struct FfnArgs {
