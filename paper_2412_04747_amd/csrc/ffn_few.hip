@@ -269,7 +269,7 @@ bool ffn_few(const rgnn_ffn_desc_t* d, bool backward) {
     const int chunks = ffn_chunks(d);
     if (backward) {
         if (d->width == 32) return d->rows <= (f32 ? chunks <= 8 ? 32768 : 12288 : chunks == 1 ? 32768 : 8192);
-        return d->rows <= (f32 ? d->width == 64 ? 8192 : 6144 : d->width == 64 ? 3584 : 3072);
+        return d->rows <= (f32 ? d->width == 64 ? 8192 : 6144 : d->width == 64 ? 3584 : 2944);
     }
     if (single(d)) return true;
     if (chunks <= kept_together(d, false)) return d->rows <= 32768 && (chunks == 1 || chunks * d->width * (f32 ? 3 : 1) <= 192);
