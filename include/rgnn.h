@@ -379,6 +379,70 @@ rgnn_status_t rgnn_norm_fwd(const rgnn_norm_desc_t* desc, const void* x, const v
 rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const float* weight, const void* dOut, const void* dSum,
                             void* dX, void* dResidual, float* dWeight, void* workspace, void* stream);
 
+/* Rows in 8 bits, for what a backward pass reads again: every 32 columns of a row (the last such block may be short) share a power of two, and a
+ * value is a whole number from -127 to 127 times it, the nearest (ties to even) to the value it stands for:
+ *   x ~ code * 2^(scale - 133),   off by at most half a step;   codes int8 [rows, width], scales uint8 [rows, ceil(width / 32)]
+ * The step is the least power of two, 2^-126 or more, with which the largest of the block rounds to at most 127; within half a step of 2^128, where
+ * there is no larger scale, it is cut to 127.  An infinity or NaN makes its block NaN (scale 255).  Unpacked values are exact in either type. */
+typedef struct {
+    int8_t* codes;               /* 16-byte aligned */
+    uint8_t* scales;
+} rgnn_rows8_t;
+typedef struct {
+    int64_t rows;                /* below 2^31 */
+    int32_t width;               /* 1 .. 8192 */
+    int32_t dtype;               /* of x */
+} rgnn_rows8_desc_t;
+/* x [rows, width] and the tensors of rows8 may not share memory. */
+rgnn_status_t rgnn_rows8_pack(const rgnn_rows8_desc_t* desc, const void* x, const rgnn_rows8_t* to, void* stream);
+rgnn_status_t rgnn_rows8_unpack(const rgnn_rows8_desc_t* desc, const rgnn_rows8_t* from, void* x, void* stream);
+
+/* Where a block's output joins the residual stream: norm after the block, gate and residual scale, norm before the next block.
+ *   n = a / sqrt(mean(a^2) + eps) * w_after;   sum = scale[t] * s + gate[t] * n;   out = sum / sqrt(mean(sum^2) + eps) * w_before
+ * row by row, t = types[row].  HGT's learned skip connection is gate[t] = sigmoid(p[t]), scale[t] = 1 - sigmoid(p[t]); a layer scale is one gate row.
+ * a_dtype: a, dA.  sum_dtype: s, sum, dSum, dS.  out_dtype: out, dOut.  Types of tensors, sums and in-range rows as for rgnn_norm_*; parameters
+ * and their gradients are fp32.
+ *   types      1, or so many rows of gate and scale that types * (width + 12) <= 4096
+ *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: every gradient is added to) */
+typedef struct {
+    int64_t rows;                /* below 2^31 */
+    int32_t width;               /* 1 .. 8192 */
+    int32_t a_dtype, sum_dtype, out_dtype;
+    int32_t types;
+    float eps;                   /* finite, >= 0 */
+    uint32_t flags;
+} rgnn_block_norm_desc_t;
+/* Device pointers.  row_types [rows]: the type of each row, or NULL with one type.  A row whose type is not 0 .. types - 1 stands for nothing (the padding of a
+ * batch): none of its tensors is read, its rows of every result are zeros (with RGNN_FLAG_ACCUMULATE: as they were), and it is no part of
+ * a parameter's gradient.
+ * NULL for w_after: n = a; gate [types, width], scale [types]: 1; w_before: no out (then NULL) and no dOut. */
+typedef struct {
+    const int32_t* row_types;
+    const float* w_after;
+    const float* gate;
+    const float* scale;
+    const float* w_before;
+} rgnn_block_norm_params_t;
+/* Gradients of the parameters, each NULL where it is not wanted or its parameter is not given. */
+typedef struct {
+    float* w_after;
+    float* gate;
+    float* scale;
+    float* w_before;
+} rgnn_block_norm_grads_t;
+rgnn_status_t rgnn_block_norm_workspace_bytes(const rgnn_block_norm_desc_t* desc, size_t* bwd_workspace);
+/* a, s [rows, width].  sum [rows, width], or NULL where it is not wanted; out is formed from the sum before that is rounded.  a8, s8: a and s in 8 bits as
+ * rgnn_rows8_pack gives them, for the backward (both, or both NULL).  sum and out may each be a's or s's own buffer (of the same type); other overlaps are not
+ * allowed. */
+rgnn_status_t rgnn_block_norm_fwd(const rgnn_block_norm_desc_t* desc, const rgnn_block_norm_params_t* params, const void* a, const void* s, void* sum,
+                                  void* out, const rgnn_rows8_t* a8, const rgnn_rows8_t* s8, void* stream);
+/* The forward's a and s, or, with a8 and s8, those instead (a and s are then NULL); sum is formed again.  dOut: gradient of out; dSum: gradient that reaches sum on
+ * its other way; either may be NULL, for zeros, but not both.  dA, dS, grads: NULL where they are not wanted; dA and dS may each be dOut's or dSum's own buffer
+ * (of the same type). */
+rgnn_status_t rgnn_block_norm_bwd(const rgnn_block_norm_desc_t* desc, const rgnn_block_norm_params_t* params, const void* a, const void* s,
+                                  const rgnn_rows8_t* a8, const rgnn_rows8_t* s8, const void* dOut, const void* dSum, void* dA, void* dS,
+                                  const rgnn_block_norm_grads_t* grads, void* workspace, void* stream);
+
 /* Gated feed-forward block, row by row, with no tensor of the hidden width in memory:
  *   out = (act(X Wg) * (X Wu)) Wd
  * X, out [rows, width]; Wg, Wu [width, hidden]; Wd [hidden, width]; every tensor, gradients too, of type dtype.
@@ -404,6 +468,10 @@ rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X, const voi
  * the forward keeps nothing. */
 rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
                            void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream);
+/* The same from rows held in 8 bits: X8 stands for X (rgnn_rows8_pack's, of rows of desc.width); the gradients are those of the values that the codes stand for,
+ * and desc.dtype is the type of every other tensor.  In RGNN_F32 these values need one bfloat16 plane instead of three. */
+rgnn_status_t rgnn_ffn_bwd_rows8(const rgnn_ffn_desc_t* desc, const rgnn_rows8_t* X8, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
+                                 void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream);
 
 /* Global norm of a model's gradients and clipping by it:
  *   norm = sqrt(sum over all tensors of the sum of g^2);   clipped = g * min(1, max_norm / (norm + 1e-6))

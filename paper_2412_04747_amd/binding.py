@@ -38,7 +38,8 @@ EXPORTS = ["rgnn_last_error", "rgnn_graph_create", "rgnn_graph_destroy", "rgnn_g
            "rgnn_workspace_bytes", "rgnn_rgcn_fwd", "rgnn_rgcn_bwd", "rgnn_rgat_fwd", "rgnn_rgat_bwd",
            "rgnn_hgt_fwd", "rgnn_hgt_bwd", "rgnn_profile_start", "rgnn_profile_stop", "rgnn_profile_select", "rgnn_rgat_fwd_static", "rgnn_schedule",
            "rgnn_norm_workspace_bytes", "rgnn_norm_fwd", "rgnn_norm_bwd", "rgnn_ffn_workspace_bytes", "rgnn_ffn_fwd", "rgnn_ffn_bwd",
-           "rgnn_clip_workspace_bytes", "rgnn_clip_grad_norm"]
+           "rgnn_clip_workspace_bytes", "rgnn_clip_grad_norm", "rgnn_rows8_pack", "rgnn_rows8_unpack", "rgnn_ffn_bwd_rows8",
+           "rgnn_block_norm_workspace_bytes", "rgnn_block_norm_fwd", "rgnn_block_norm_bwd"]
 
 
 class RgnnError(RuntimeError):
@@ -69,6 +70,27 @@ class FfnDesc(C.Structure):
                 ("flags", C.c_uint32)]
 
 
+class Rows8Desc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32)]
+
+
+class Rows8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
+class BlockNormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int32), ("a_dtype", C.c_int32), ("sum_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("types", C.c_int32), ("eps", C.c_float), ("flags", C.c_uint32)]
+
+
+class BlockNormParams(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("row_types", "w_after", "gate", "scale", "w_before")]
+
+
+class BlockNormGrads(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("w_after", "gate", "scale", "w_before")]
+
+
 class Schedule(C.Structure):
     _fields_ = [(k, C.c_int32) for k in (
         "item_len", "tile_chunks", "wide_chunks", "rows_bf16", "row_select", "hgt_folded", "fused_softmax", "ws_in_lds",
@@ -84,7 +106,9 @@ _P = C.c_void_p
 _ROW_OPS = {"rgnn_norm_workspace_bytes": [_P] * 2, "rgnn_norm_fwd": [_P] * 7, "rgnn_norm_bwd": [_P] * 10,
             "rgnn_ffn_workspace_bytes": [_P] * 3, "rgnn_ffn_fwd": [_P] * 8, "rgnn_ffn_bwd": [_P] * 12,
             "rgnn_clip_workspace_bytes": [C.c_int64, _P, _P],
-            "rgnn_clip_grad_norm": [C.c_int64, _P, _P, _P, _P, C.c_float, _P, _P, _P]}
+            "rgnn_clip_grad_norm": [C.c_int64, _P, _P, _P, _P, C.c_float, _P, _P, _P],
+            "rgnn_ffn_bwd_rows8": [_P] * 12, "rgnn_rows8_pack": [_P] * 4, "rgnn_rows8_unpack": [_P] * 4, "rgnn_block_norm_workspace_bytes": [_P] * 2,
+            "rgnn_block_norm_fwd": [_P] * 9, "rgnn_block_norm_bwd": [_P] * 13}
 
 _lib = None
 
@@ -244,6 +268,59 @@ def rgnn_ffn_fwd(desc, X, Wg, Wu, Wd, out, workspace, stream=None):
 def rgnn_ffn_bwd(desc, X, Wg, Wu, Wd, dOut, dX, dWg, dWu, dWd, workspace, stream=None):
     _check(lib().rgnn_ffn_bwd(C.byref(desc), _addr(X), _addr(Wg), _addr(Wu), _addr(Wd), _addr(dOut), _addr(dX), _addr(dWg), _addr(dWu),
                               _addr(dWd), _addr(workspace), stream))
+
+
+def make_rows8_desc(rows, width, dtype=RGNN_F32):
+    return Rows8Desc(rows, width, dtype)
+
+
+def rows8(codes, scales):
+    """The pair of tensors (or addresses) as the calls take it."""
+    return Rows8(_addr(codes), _addr(scales))
+
+
+def _ref(struct):
+    return None if struct is None else C.byref(struct)
+
+
+def rgnn_ffn_bwd_rows8(desc, X8, Wg, Wu, Wd, dOut, dX, dWg, dWu, dWd, workspace, stream=None):
+    _check(lib().rgnn_ffn_bwd_rows8(C.byref(desc), _ref(X8), _addr(Wg), _addr(Wu), _addr(Wd), _addr(dOut), _addr(dX), _addr(dWg), _addr(dWu),
+                                    _addr(dWd), _addr(workspace), stream))
+
+
+def rgnn_rows8_pack(desc, x, to, stream=None):
+    _check(lib().rgnn_rows8_pack(C.byref(desc), _addr(x), _ref(to), stream))
+
+
+def rgnn_rows8_unpack(desc, source, x, stream=None):
+    _check(lib().rgnn_rows8_unpack(C.byref(desc), _ref(source), _addr(x), stream))
+
+
+def make_block_norm_desc(rows, width, a_dtype=RGNN_F32, sum_dtype=RGNN_F32, out_dtype=RGNN_F32, types=1, eps=1e-6, flags=0):
+    return BlockNormDesc(rows, width, a_dtype, sum_dtype, out_dtype, types, eps, flags)
+
+
+def block_norm_params(row_types=None, w_after=None, gate=None, scale=None, w_before=None):
+    return BlockNormParams(*map(_addr, (row_types, w_after, gate, scale, w_before)))
+
+
+def block_norm_grads(w_after=None, gate=None, scale=None, w_before=None):
+    return BlockNormGrads(*map(_addr, (w_after, gate, scale, w_before)))
+
+
+def rgnn_block_norm_workspace_bytes(desc):
+    b = C.c_size_t()
+    _check(lib().rgnn_block_norm_workspace_bytes(C.byref(desc), C.byref(b)))
+    return b.value
+
+
+def rgnn_block_norm_fwd(desc, params, a, s, sum, out, a8=None, s8=None, stream=None):
+    _check(lib().rgnn_block_norm_fwd(C.byref(desc), _ref(params), _addr(a), _addr(s), _addr(sum), _addr(out), _ref(a8), _ref(s8), stream))
+
+
+def rgnn_block_norm_bwd(desc, params, a, s, a8, s8, dOut, dSum, dA, dS, grads, workspace, stream=None):
+    _check(lib().rgnn_block_norm_bwd(C.byref(desc), _ref(params), _addr(a), _addr(s), _ref(a8), _ref(s8), _addr(dOut), _addr(dSum), _addr(dA),
+                                     _addr(dS), _ref(grads), _addr(workspace), stream))
 
 
 def rgnn_clip_workspace_bytes(sizes):

@@ -10,6 +10,7 @@
 #include <math.h>
 
 #include "row_ops.h"
+#include "rows8.h"
 
 namespace rgnn {
 
@@ -27,7 +28,11 @@ struct FfnArgs {
     int64_t rows;
     int hidden, chunks;                  // chunks = ceil(hidden / kHid)
     const void* X; const void* Wg; const void* Wu; const void* Wd; const void* dOut;
+    const uint8_t* x_scales;             // X held in 8 bits: X is its codes
 };
+
+// Planes of X: rows held in 8 bits are exact in one.
+constexpr int x_planes(int planes, bool held) { return held ? 1 : planes; }
 
 // planes of eight values: PL == 1 rounds to bfloat16; PL == 2 keeps 16 bits, PL == 3 is exact to 24: x = hi + mid + lo (each rounded to nearest even)
 template <int PL>
@@ -59,6 +64,11 @@ template <typename Acc>
 __device__ __forceinline__ void mul_add(const bf16x8 (&a)[1], const bf16x8 (&b)[1], Acc& c) { c = mfma(a[0], b[0], c); }
 template <typename Acc>
 __device__ __forceinline__ void mul_add(const bf16x8 (&a)[1], const bf16x8 (&b)[2], Acc& c) { c = mfma(a[0], b[0], mfma(a[0], b[1], c)); }
+// (three planes and one that is exact: all three products)
+template <typename Acc>
+__device__ __forceinline__ void mul_add(const bf16x8 (&a)[3], const bf16x8 (&b)[1], Acc& c) { c = mfma(a[0], b[0], mfma(a[1], b[0], mfma(a[2], b[0], c))); }
+template <typename Acc>
+__device__ __forceinline__ void mul_add(const bf16x8 (&a)[1], const bf16x8 (&b)[3], Acc& c) { c = mfma(a[0], b[0], mfma(a[0], b[1], mfma(a[0], b[2], c))); }
 template <typename Acc>
 __device__ __forceinline__ void mul_add(const bf16x8 (&a)[3], const bf16x8 (&b)[3], Acc& c) {
     c = mfma(a[0], b[2], c);
@@ -110,6 +120,31 @@ __device__ __forceinline__ void load_planes8(const T* X, int64_t row, int64_t ro
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = ok ? v[e] : 0.f;
         planes8<PL>(v, f);
+    }
+}
+
+// Values of 8 bits as bfloat16, two to a word.
+template <int V>
+__device__ __forceinline__ void held_words(const CodeWords<V>& w, unsigned scale, unsigned (&q)[V / 2]) {
+    float v[V];
+    from_codes<V>(w, held_step(scale), v);
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) q[e] = bf16_pack2(v[2 * e], v[2 * e + 1]);
+}
+// The columns of X that load_planes8 takes, from the rows as they are given or from their 8 bits.
+template <int D, int PL, bool HELD, typename T, int XP>
+__device__ __forceinline__ void load_x8(const FfnArgs& a, int64_t row, int col, bf16x8 (&f)[XP]) {
+    if constexpr (HELD) {
+        const bool ok = row < a.rows;
+        const int64_t at = ok ? row : a.rows - 1;
+        CodeWords<8> w;
+        load_codes<true, 8>(static_cast<const int8_t*>(a.X) + at * D, col, D, w);
+        const unsigned b = a.x_scales[at * (D / kHeldBlock) + col / kHeldBlock];
+        unsigned q[4];
+        held_words<8>(w, ok ? b : 0, q);
+        f[0] = __builtin_bit_cast(bf16x8, make_uint4(q[0], q[1], q[2], q[3]));
+    } else {
+        load_planes8<D, PL>(static_cast<const T*>(a.X), row, a.rows, col, f);
     }
 }
 
@@ -245,7 +280,8 @@ inline int ffn_grad_shares(const rgnn_ffn_desc_t* d, int most) {
 bool ffn_few(const rgnn_ffn_desc_t* d, bool backward);
 size_t ffn_few_bytes(const rgnn_ffn_desc_t* d, bool backward);
 rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out, void* workspace, hipStream_t st);
-rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st);
+// held: X in 8 bits
+rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, bool held, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st);
 
 #define RGNN_DISPATCH_FFN(DESC, ...)                                                                                   \
     do {                                                                                                               \

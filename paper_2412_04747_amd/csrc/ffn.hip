@@ -60,12 +60,12 @@ __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, false>::per_simd)) 
 // The backward's two passes in one launch: workgroups [0, row_blocks) take the rows, the others the weights' gradients.  Neither waits for
 // the other's last workgroups (either by itself, in sum / both in one: 14000 rows, d 64, f 256, bf16, 37.3 / 26.6 us; 200017 rows, d 128, f 341, 322 / 300;
 // 1M rows, d 64, f 256, 605 / 592; fp32, 1832 / 1858).
-template <int D, int PL, int ACT>
+template <int D, int PL, int ACT, bool HELD>
 __global__ __launch_bounds__(64 * kRowWaves, (RowsCut<D, PL, true>::per_simd)) void ffn_bwd_kernel(RowsArgs r, FfnGradArgs k, int row_blocks) {
     extern __shared__ unsigned char lds[];
     const int b = (int)blockIdx.x - row_blocks;
-    if (b < 0) rows_block<D, PL, ACT, true>(r, blockIdx.x, lds);
-    else grad_block<D, PL, ACT, false>(k, b % k.splits, b / k.splits, lds);
+    if (b < 0) rows_block<D, PL, ACT, true, 1, HELD>(r, blockIdx.x, lds);
+    else grad_block<D, PL, ACT, false, HELD>(k, b % k.splits, b / k.splits, lds);
 }
 
 template <typename T>
@@ -126,7 +126,7 @@ rgnn_status_t grad_reduce(const rgnn_ffn_desc_t* d, const FfnGradArgs& k, hipStr
 }
 
 // dX or the weights' gradients may be null; the other's are the same either way.
-rgnn_status_t backward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, int accumulate, void* workspace, hipStream_t st) {
+rgnn_status_t backward(const rgnn_ffn_desc_t* d, const FfnArgs& a, bool held, void* dX, void* dWg, void* dWu, void* dWd, int accumulate, void* workspace, hipStream_t st) {
     unsigned char* const packed = static_cast<unsigned char*>(workspace);
     const RowsArgs r{a, packed, dX, nullptr, 1, accumulate};
     const FfnGradArgs k{a, reinterpret_cast<float*>(packed + packed_bytes(d, true)), grad_splits(d), ffn_grad_groups(d), dWg, dWu, dWd, accumulate};
@@ -135,7 +135,7 @@ rgnn_status_t backward(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, voi
         RGNN_DISPATCH_FFN(d, {
             if (rows) RGNN_TRY((launch_pack<D, PL>(a, true, packed, st)));
             constexpr size_t lds = std::max(Weights<D, PL, true>::lds, (size_t)Cut<D, PL>::lds);
-            auto* const kernel = ffn_bwd_kernel<D, PL, ACT>;
+            auto* const kernel = held ? ffn_bwd_kernel<D, PL, ACT, true> : ffn_bwd_kernel<D, PL, ACT, false>;
             RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
             KernelTimer timer(st, "ffn_bwd");
             kernel<<<rows + grads, 64 * kRowWaves, lds, st>>>(r, k, rows);
@@ -196,28 +196,51 @@ extern "C" rgnn_status_t rgnn_ffn_fwd(const rgnn_ffn_desc_t* desc, const void* X
     const int32_t t = desc->dtype;
     RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t)},
                            {span(out, n, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, false)}}));
-    const FfnArgs a{desc->rows, desc->hidden, ffn_chunks(desc), X, Wg, Wu, Wd, nullptr};
+    const FfnArgs a{desc->rows, desc->hidden, ffn_chunks(desc), X, Wg, Wu, Wd, nullptr, nullptr};
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return ffn_few(desc, false) ? ffn_few_fwd(desc, a, out, workspace, st) : forward(desc, a, out, workspace, st);
 }
 
-extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
-                                      void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream) {
-    RGNN_TRY(check_desc(desc));
+namespace rgnn {
+namespace {
+
+// The backward; held: X in 8 bits, given for X.
+rgnn_status_t ffn_backward(const rgnn_ffn_desc_t* desc, const void* X, const rgnn_rows8_t* held, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
+                           void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream) {
     const bool grads = dWg || dWu || dWd;
     if (grads && !(dWg && dWu && dWd)) RGNN_FAIL(RGNN_EINVAL, "dWg, dWu and dWd are given together or not at all");
     if (!Wg || !Wu || !Wd) RGNN_FAIL(RGNN_EINVAL, "a weight is NULL");
-    if (desc->rows > 0 && (!X || !dOut)) RGNN_FAIL(RGNN_EINVAL, "X or dOut is NULL");
+    if (desc->rows > 0 && (!X || !dOut || (held && !held->scales))) RGNN_FAIL(RGNN_EINVAL, "X or dOut is NULL");
     if (!workspace) RGNN_FAIL(RGNN_EWORKSPACE, "workspace is NULL");
     const size_t n = (size_t)desc->rows * desc->width, w = (size_t)desc->hidden * desc->width;
     const int32_t t = desc->dtype;
-    RGNN_TRY(check_tensors({span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t), span(dOut, n, t)},
-                           {span(dX, n, t), span(dWg, w, t), span(dWu, w, t), span(dWd, w, t), Span{static_cast<char*>(workspace), workspace_bytes(desc, true)}}));
+    const std::initializer_list<Span> written{span(dX, n, t), span(dWg, w, t), span(dWu, w, t), span(dWd, w, t),
+                                              Span{static_cast<char*>(workspace), workspace_bytes(desc, true)}};
+    RGNN_TRY(check_tensors({held ? code_span(held, desc->rows, desc->width) : span(X, n, t), span(Wg, w, t), span(Wu, w, t), span(Wd, w, t), span(dOut, n, t)}, written));
+    if (held)
+        for (const Span& s : written)
+            if (s.overlaps(scale_span(held, desc->rows, desc->width))) RGNN_FAIL(RGNN_EINVAL, "an output or the workspace overlaps the scales of X");
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const FfnArgs a{desc->rows, desc->hidden, ffn_chunks(desc), X, Wg, Wu, Wd, dOut};
+    const FfnArgs a{desc->rows, desc->hidden, ffn_chunks(desc), X, Wg, Wu, Wd, dOut, held ? held->scales : nullptr};
     const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
-    if (desc->rows > 0 && ffn_few(desc, true)) return ffn_few_bwd(desc, a, dX, dWg, dWu, dWd, workspace, st);
+    if (desc->rows > 0 && ffn_few(desc, true)) return ffn_few_bwd(desc, a, held, dX, dWg, dWu, dWd, workspace, st);
     if (desc->rows == 0) dX = nullptr;
     if (!grads || (desc->rows == 0 && accumulate)) dWg = nullptr;
-    return backward(desc, a, dX, dWg, dWu, dWd, accumulate, workspace, st);
+    return backward(desc, a, held, dX, dWg, dWu, dWd, accumulate, workspace, st);
+}
+
+}  // namespace
+}  // namespace rgnn
+
+extern "C" rgnn_status_t rgnn_ffn_bwd(const rgnn_ffn_desc_t* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
+                                      void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream) {
+    RGNN_TRY(check_desc(desc));
+    return ffn_backward(desc, X, nullptr, Wg, Wu, Wd, dOut, dX, dWg, dWu, dWd, workspace, stream);
+}
+
+extern "C" rgnn_status_t rgnn_ffn_bwd_rows8(const rgnn_ffn_desc_t* desc, const rgnn_rows8_t* X8, const void* Wg, const void* Wu, const void* Wd, const void* dOut,
+                                            void* dX, void* dWg, void* dWu, void* dWd, void* workspace, void* stream) {
+    RGNN_TRY(check_desc(desc));
+    if (!X8) RGNN_FAIL(RGNN_EINVAL, "X8 is NULL");
+    return ffn_backward(desc, X8->codes, X8, Wg, Wu, Wd, dOut, dX, dWg, dWu, dWd, workspace, stream);
 }

@@ -18,18 +18,19 @@ namespace {
 template <int D, int PL, bool BWD> constexpr int rows_lds() { return (BWD ? 5 : 3) * (D / 16) * PL * kFrag; }
 
 // 128 rows, a share of the chunks.
-template <int D, int PL, int ACT, bool BWD>
+template <int D, int PL, int ACT, bool BWD, bool HELD = false>
 __device__ __forceinline__ void few_rows_block(const RowsArgs& r, int block, int split, unsigned char* lds) {
-    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves, HP = hidden_planes(PL);
+    constexpr int S = D / 16, TILES = D / 32, SECTIONS = BWD ? 5 : 3, EACH = (S + kRowWaves - 1) / kRowWaves, HP = hidden_planes(PL),
+                  XP = x_planes(PL, HELD);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
     const int64_t row0 = ((int64_t)block * kRowWaves + wave) * 32, row = row0 + m;
     const int c0 = (int)((int64_t)r.a.chunks * split / r.splits), c1 = (int)((int64_t)r.a.chunks * (split + 1) / r.splits);
-    bf16x8 x[S][PL], dy[BWD ? S : 1][PL];
+    bf16x8 x[S][XP], dy[BWD ? S : 1][PL];
     v16f y[TILES];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        load_planes8<D, PL>(static_cast<const T*>(r.a.X), row, r.a.rows, 16 * s + 8 * kh, x[s]);
+        load_x8<D, PL, HELD, T>(r.a, row, 16 * s + 8 * kh, x[s]);
         if constexpr (BWD) load_planes8<D, PL>(static_cast<const T*>(r.a.dOut), row, r.a.rows, 16 * s + 8 * kh, dy[s]);
     }
 #pragma unroll
@@ -182,16 +183,16 @@ __global__ __launch_bounds__(256) void ffn_single_fwd_kernel(RowsArgs r) {
 }
 
 // Workgroups [0, row_blocks * r.splits) form dX, the others the weights' gradients.
-template <int D, int PL, int ACT>
+template <int D, int PL, int ACT, bool HELD>
 __global__ __launch_bounds__(64 * kRowWaves, 1) void ffn_few_bwd_kernel(RowsArgs r, FfnGradArgs k, int row_blocks) {
     extern __shared__ unsigned char lds[];
     const int b = blockIdx.x, n = row_blocks * r.splits;
     if (b < n) {
-        few_rows_block<D, PL, ACT, true>(r, b % row_blocks, b / row_blocks, lds);
+        few_rows_block<D, PL, ACT, true, HELD>(r, b % row_blocks, b / row_blocks, lds);
     } else if (k.splits == 1) {
-        grad_block<D, PL, ACT, true>(k, 0, b - n, lds);
+        grad_block<D, PL, ACT, true, HELD>(k, 0, b - n, lds);
     } else {
-        grad_block<D, PL, ACT, false>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
+        grad_block<D, PL, ACT, false, HELD>(k, (b - n) % k.splits, (b - n) / k.splits, lds);
     }
 }
 
@@ -304,7 +305,7 @@ rgnn_status_t ffn_few_fwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* out,
     return sum(d, r, k, st);
 }
 
-rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st) {
+rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, bool held, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, hipStream_t st) {
     const int accumulate = (d->flags & RGNN_FLAG_ACCUMULATE) != 0;
     RowsArgs r{a, nullptr, dX, static_cast<float*>(workspace), row_splits(d, true), accumulate};
     FfnGradArgs k{a, reinterpret_cast<float*>(static_cast<char*>(workspace) + share_bytes(d, true)), few_grad_splits(d), ffn_grad_groups(d), dWg, dWu, dWd, accumulate};
@@ -313,7 +314,7 @@ rgnn_status_t ffn_few_bwd(const rgnn_ffn_desc_t* d, const FfnArgs& a, void* dX, 
     auto run = [&]() -> rgnn_status_t {
         RGNN_DISPATCH_FFN(d, {
             constexpr int lds = std::max(rows_lds<D, PL, true>(), Cut<D, PL>::lds);
-            auto* const kernel = ffn_few_bwd_kernel<D, PL, ACT>;
+            auto* const kernel = held ? ffn_few_bwd_kernel<D, PL, ACT, true> : ffn_few_bwd_kernel<D, PL, ACT, false>;
             RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
             KernelTimer timer(st, "ffn_few_bwd");
             kernel<<<rows * r.splits + grads, 64 * kRowWaves, lds, st>>>(r, k, rows);

@@ -17,9 +17,9 @@ namespace rgnn {
 
 constexpr int UNIT = 32;
 
-template <int D, int PL> struct Cut {
+template <int D, int PL, bool HELD = false> struct Cut {
     static constexpr int MT = PL == 1 && D < 128 ? 32 : 16;      // hidden values of a wavefront
-    static constexpr int lds = 2 * 2 * PL * UNIT * D * 2;        // two units of either tensor
+    static constexpr int lds = 2 * (x_planes(PL, HELD) + PL) * UNIT * D * 2;        // two units of either tensor
 };
 struct FfnGradArgs {
     FfnArgs a;
@@ -37,14 +37,14 @@ __device__ __forceinline__ int swizzle(int r) {
 }
 
 // The workgroup's share of the rows, `split`, and of the hidden values, `group`.
-template <int D, int PL, int ACT, bool DIRECT>
+template <int D, int PL, int ACT, bool DIRECT, bool HELD = false>
 __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int group, unsigned char* lds) {
-    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves, HP = hidden_planes(PL);
+    constexpr int MT = Cut<D, PL>::MT, WAVES = kRowWaves, HP = hidden_planes(PL), XP = x_planes(PL, HELD);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     using Acc = typename std::conditional<MT == 32, v16f, v4f>::type;
     constexpr int KS = MT == 32 ? 16 : 32;               // contraction of an instruction
     constexpr int S = D / KS, NR = MT == 32 ? 16 : 4, RTS = UNIT / MT, STEPS = UNIT / KS, TILES = D / MT;
-    constexpr int PLANE = UNIT * D * 2, BUF = 2 * PL * PLANE;
+    constexpr int PLANE = UNIT * D * 2, BUF = (XP + PL) * PLANE;
     // pieces of V columns (16 bytes, or 8 where the unit has fewer than the threads) that a thread loads of either tensor
     constexpr int V = PL == 3 || UNIT * D / 8 < 64 * WAVES ? 4 : 8, PIECES = UNIT * D / V, ITEMS = (PIECES + 64 * WAVES - 1) / (64 * WAVES);
     using Raw = typename std::conditional<sizeof(T) * V == 16, rgnn_v4u, rgnn_v2u>::type;
@@ -80,15 +80,29 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
     }
 
     const int64_t units = (a.rows + UNIT - 1) / UNIT;
-    Raw xr[ITEMS], yr[ITEMS];
+    Raw xr[HELD ? 1 : ITEMS], yr[ITEMS];
+    CodeWords<V> codes[HELD ? ITEMS : 1];
+    unsigned scales[HELD ? ITEMS : 1];
     auto load = [&](int64_t u) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int at = threadIdx.x + i * 64 * WAVES, rr = at / (D / V), c = at % (D / V) * V;
             const int64_t row = u * UNIT + rr;
-            xr[i] = yr[i] = Raw{};
+            yr[i] = Raw{};
+            if constexpr (HELD) {
+                scales[i] = 0;
+#pragma unroll
+                for (int q = 0; q < V / 4; ++q) codes[i][q] = 0;
+            } else {
+                xr[i] = Raw{};
+            }
             if (at < PIECES && row < a.rows) {
-                xr[i] = *reinterpret_cast<const Raw*>(static_cast<const T*>(a.X) + row * D + c);
+                if constexpr (HELD) {
+                    load_codes<true, V>(static_cast<const int8_t*>(a.X) + row * D, c, D, codes[i]);
+                    scales[i] = a.x_scales[row * (D / kHeldBlock) + c / kHeldBlock];
+                } else {
+                    xr[i] = *reinterpret_cast<const Raw*>(static_cast<const T*>(a.X) + row * D + c);
+                }
                 yr[i] = *reinterpret_cast<const Raw*>(static_cast<const T*>(a.dOut) + row * D + c);
             }
         }
@@ -99,14 +113,19 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
             const int at = threadIdx.x + i * 64 * WAVES, rr = at / (D / V), c = at % (D / V) * V;
             if (PIECES % (64 * WAVES) && at >= PIECES) break;
             unsigned char* const p = buf + rr * (2 * D) + (((c >> 3) ^ swizzle<D>(rr)) << 4) + (c & 4) * 2;
+            if constexpr (HELD) {
+                unsigned q[V / 2];
+                held_words<V>(codes[i], scales[i], q);
+                __builtin_memcpy(__builtin_assume_aligned(p, 2 * V), q, sizeof(q));
+            }
             if constexpr (PL == 1) {
-                *reinterpret_cast<Raw*>(p) = xr[i];
+                if constexpr (!HELD) *reinterpret_cast<Raw*>(p) = xr[i];
                 *reinterpret_cast<Raw*>(p + PLANE) = yr[i];
             } else {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = __uint_as_float(xr[i][e]);
+                    v[e] = HELD ? 0.f : __uint_as_float(xr[HELD ? 0 : i][e]);
                     v[4 + e] = __uint_as_float(yr[i][e]);
                 }
                 bf16x8 q[PL];
@@ -114,8 +133,8 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
 #pragma unroll
                 for (int l = 0; l < PL; ++l) {
                     const uint4 w = __builtin_bit_cast(uint4, q[l]);
-                    *reinterpret_cast<uint2*>(p + l * PLANE) = make_uint2(w.x, w.y);
-                    *reinterpret_cast<uint2*>(p + (PL + l) * PLANE) = make_uint2(w.z, w.w);
+                    if constexpr (!HELD) *reinterpret_cast<uint2*>(p + l * PLANE) = make_uint2(w.x, w.y);
+                    *reinterpret_cast<uint2*>(p + (XP + l) * PLANE) = make_uint2(w.z, w.w);
                 }
             }
         }
@@ -126,17 +145,17 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
     const int rows_at = m * (2 * D) + ((kg ^ swizzle<D>(m)) << 4);
     const int cols_at = (tr & 15) * (2 * D) + (((2 * half + ((i16 & 3) >> 1)) ^ swizzle<D>(tr)) << 4) + (i16 & 1) * 8;
     // rows of tile i, columns KS s + 8 kg ..: of X (which = 0) or dOut (1)
-    auto rows_operand = [&](const unsigned char* buf, int at, int which, int i, int s, bf16x8 (&f)[PL]) {
-        const unsigned char* const p = buf + ((at ^ (KS * 2 * s)) + i * MT * 2 * D + which * PL * PLANE);
+    auto rows_operand = [&](const unsigned char* buf, int at, int which, int i, int s, auto& f) {
+        const unsigned char* const p = buf + ((at ^ (KS * 2 * s)) + i * MT * 2 * D + which * XP * PLANE);
 #pragma unroll
-        for (int l = 0; l < PL; ++l) f[l] = *reinterpret_cast<const bf16x8*>(p + l * PLANE);
+        for (int l = 0; l < (int)(sizeof(f) / 16); ++l) f[l] = *reinterpret_cast<const bf16x8*>(p + l * PLANE);
     };
     // columns MT t + m, the rows in the order of the accumulators' values 8 s ..: rows 16 s + 4 kg .. and 8 further, or 4 kg .. and 16 further
-    auto cols_operand = [&](const unsigned char* buf, int at, int which, int t, int s, bf16x8 (&f)[PL]) {
-        const int p = (at ^ (MT * 2 * t)) + s * 16 * 2 * D + which * PL * PLANE;
-        const int q = (at ^ (MT * 2 * t) ^ (MT == 32 ? 16 : 0)) + s * 16 * 2 * D + which * PL * PLANE + (MT == 32 ? 8 : 16) * 2 * D;
+    auto cols_operand = [&](const unsigned char* buf, int at, int which, int t, int s, auto& f) {
+        const int p = (at ^ (MT * 2 * t)) + s * 16 * 2 * D + which * XP * PLANE;
+        const int q = (at ^ (MT * 2 * t) ^ (MT == 32 ? 16 : 0)) + s * 16 * 2 * D + which * XP * PLANE + (MT == 32 ? 8 : 16) * 2 * D;
 #pragma unroll
-        for (int l = 0; l < PL; ++l) f[l] = tr8(buf + p + l * PLANE, buf + q + l * PLANE);
+        for (int l = 0; l < (int)(sizeof(f) / 16); ++l) f[l] = tr8(buf + p + l * PLANE, buf + q + l * PLANE);
     };
 
     int64_t u = split;
@@ -158,10 +177,10 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
             clear(dh[i]);
 #pragma unroll
             for (int s = 0; s < S; ++s) {
-                bf16x8 f[PL];
-                rows_operand(buf, ra, 0, i, s, f);
-                mul_add(f, wg[s], g[i]);
-                mul_add(f, wu[s], up[i]);
+                bf16x8 x[XP], f[PL];
+                rows_operand(buf, ra, 0, i, s, x);
+                mul_add(x, wg[s], g[i]);
+                mul_add(x, wu[s], up[i]);
                 rows_operand(buf, ra, 1, i, s, f);
                 mul_add(f, wd[s], dh[i]);
             }
@@ -189,10 +208,10 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
             if constexpr (PL == 1) {
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
-                    bf16x8 f[PL];
-                    cols_operand(buf, ca, 0, t, s, f);
-                    mul_add(f, gp[s], dwg[t]);
-                    mul_add(f, upp[s], dwu[t]);
+                    bf16x8 x[XP], f[PL];
+                    cols_operand(buf, ca, 0, t, s, x);
+                    mul_add(x, gp[s], dwg[t]);
+                    mul_add(x, upp[s], dwu[t]);
                     cols_operand(buf, ca, 1, t, s, f);
                     mul_add(f, hp[s], dwd[t]);
                 }
@@ -203,10 +222,10 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
                 clear(td);
 #pragma unroll
                 for (int s = 0; s < STEPS; ++s) {
-                    bf16x8 f[PL];
-                    cols_operand(buf, ca, 0, t, s, f);
-                    mul_add(f, gp[s], tg);
-                    mul_add(f, upp[s], tu);
+                    bf16x8 x[XP], f[PL];
+                    cols_operand(buf, ca, 0, t, s, x);
+                    mul_add(x, gp[s], tg);
+                    mul_add(x, upp[s], tu);
                     cols_operand(buf, ca, 1, t, s, f);
                     mul_add(f, hp[s], td);
                 }

@@ -42,11 +42,11 @@ template <int D, int PL, bool BWD> struct RowsCut {
 
 // 128 rows, all chunks.  GROUPS > 1: 128 / GROUPS rows, whose chunks are divided among the groups of wavefronts, each with places in the LDS of its own; the
 // shares are added through the LDS, in order.
-template <int D, int PL, int ACT, bool BWD, int GROUPS = 1>
+template <int D, int PL, int ACT, bool BWD, int GROUPS = 1, bool HELD = false>
 __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, unsigned char* lds) {
     using W = Weights<D, PL, BWD>;
     using Cut = RowsCut<D, PL, BWD>;
-    constexpr int S = D / 16, TILES = D / 32, HP = hidden_planes(PL);
+    constexpr int S = D / 16, TILES = D / 32, HP = hidden_planes(PL), XP = x_planes(PL, HELD);
     using T = typename std::conditional<PL == 1, bf16_t, float>::type;
     constexpr int WAVES = kRowWaves / GROUPS;
     const int wave = (threadIdx.x >> 6) & (WAVES - 1), lane = threadIdx.x & 63, m = lane & 31, kh = lane >> 5;
@@ -63,11 +63,11 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
         if (Cut::ahead) fetch_first(c0 + 1);
         fetch_second(c0);
     }
-    bf16x8 x[S][PL], dy[BWD ? S : 1][PL];
+    bf16x8 x[S][XP], dy[BWD ? S : 1][PL];
     v16f y[TILES];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-        load_planes8<D, PL>(static_cast<const T*>(r.a.X), row, r.a.rows, 16 * s + 8 * kh, x[s]);
+        load_x8<D, PL, HELD, T>(r.a, row, 16 * s + 8 * kh, x[s]);
         if constexpr (BWD) load_planes8<D, PL>(static_cast<const T*>(r.a.dOut), row, r.a.rows, 16 * s + 8 * kh, dy[s]);
     }
 #pragma unroll

@@ -217,8 +217,70 @@ class NormLayer:
         B.rgnn_norm_bwd(self.desc, self.sum, self.weight, self.dOut, self.dSum, self.dX, self.dResidual, self.dWeight, self.ws, _stream())
 
 
+_ROW_TYPES = {torch.float32: B.RGNN_F32, torch.bfloat16: B.RGNN_BF16}
+
+
+class Rows8:
+    """Buffers for `rows` rows held in 8 bits: `codes` int8 [rows, width], `scales` uint8 [rows, blocks of 32 columns].  Both may be replaced by the
+    caller's own."""
+
+    def __init__(self, rows, width):
+        self.rows, self.width = rows, width
+        self.codes = torch.empty(rows, width, device="cuda", dtype=torch.int8)
+        self.scales = torch.empty(rows, -(-width // 32), device="cuda", dtype=torch.uint8)
+        self._descs = {t: B.make_rows8_desc(rows, width, code) for t, code in _ROW_TYPES.items()}
+
+    def _desc(self, x):
+        if x.dtype not in self._descs or not x.is_cuda or not x.is_contiguous() or x.numel() != self.rows * self.width:
+            raise TypeError(f"Rows8: {self.rows} contiguous rows of {self.width} in fp32 or bf16 on the GPU are wanted, not {tuple(x.shape)} in {x.dtype}")
+        return self._descs[x.dtype]
+
+    def tensors(self):
+        return B.rows8(self.codes, self.scales)
+
+    def pack(self, x):
+        B.rgnn_rows8_pack(self._desc(x), x, self.tensors(), _stream())
+
+    def unpack(self, x):
+        B.rgnn_rows8_unpack(self._desc(x), self.tensors(), x, _stream())
+
+
+class BlockNormLayer:
+    """Device buffers for one junction call pair on `rows` rows: norm after a block, gate and residual scale by node type, norm before the next.  `a`, `s`
+    (and `dOut`, `dSum`), the parameters and `types` (int32, with more than one) are set by the caller; types "f32" or "bf16".  held: the forward leaves
+    a and s in 8 bits (`held_a`, `held_s`), and the backward reads them there."""
+
+    def __init__(self, rows, width, a="f32", total="f32", out="f32", types=1, eps=1e-6, held=False, flags=0):
+        (ca, ta), (cs, ts), (co, to) = _tdtype(a), _tdtype(total), _tdtype(out)
+        self.desc = B.make_block_norm_desc(rows, width, ca, cs, co, types, eps, flags)
+        self.ws = _buf(B.rgnn_block_norm_workspace_bytes(self.desc))
+        e = lambda *shape, t=torch.float32: torch.empty(*shape, device="cuda", dtype=t)
+        self.types = self.w_after = self.w_before = self.gate = self.scale = None
+        self.a = self.s = self.dOut = self.dSum = None
+        self.sum, self.out, self.dA, self.dS = e(rows, width, t=ts), e(rows, width, t=to), e(rows, width, t=ta), e(rows, width, t=ts)
+        self.dWAfter, self.dWBefore, self.dGate, self.dScale = e(width), e(width), e(types, width), e(types)
+        self.held_a, self.held_s = (Rows8(rows, width), Rows8(rows, width)) if held else (None, None)
+
+    def _params(self):
+        return B.block_norm_params(self.types, self.w_after, self.gate, self.scale, self.w_before)
+
+    def _held(self):
+        return (None, None) if self.held_a is None else (self.held_a.tensors(), self.held_s.tensors())
+
+    def fwd(self):
+        B.rgnn_block_norm_fwd(self.desc, self._params(), self.a, self.s, self.sum, None if self.w_before is None else self.out, *self._held(), _stream())
+
+    def bwd(self):
+        a8, s8 = self._held()
+        grads = B.block_norm_grads(*(g if p is not None else None for g, p in (
+            (self.dWAfter, self.w_after), (self.dGate, self.gate), (self.dScale, self.scale), (self.dWBefore, self.w_before))))
+        a, s = (self.a, self.s) if a8 is None else (None, None)
+        B.rgnn_block_norm_bwd(self.desc, self._params(), a, s, a8, s8, self.dOut, self.dSum, self.dA, self.dS, grads, self.ws, _stream())
+
+
 class FfnLayer:
-    """Device buffers for one feed-forward block call pair on `rows` rows.  `X`, `Wg`, `Wu`, `Wd` (and `dOut`) are set by the caller."""
+    """Device buffers for one feed-forward block call pair on `rows` rows.  `X`, `Wg`, `Wu`, `Wd` (and `dOut`) are set by the caller; for `bwd_held`, the
+    backward from rows in 8 bits, `held` (Rows8) instead of `X`."""
 
     def __init__(self, rows, width, hidden, dtype="f32", act="silu", flags=0):
         code, t = _tdtype(dtype)
@@ -233,6 +295,9 @@ class FfnLayer:
 
     def bwd(self):
         B.rgnn_ffn_bwd(self.desc, self.X, self.Wg, self.Wu, self.Wd, self.dOut, self.dX, self.dWg, self.dWu, self.dWd, self.ws, _stream())
+
+    def bwd_held(self):
+        B.rgnn_ffn_bwd_rows8(self.desc, self.held.tensors(), self.Wg, self.Wu, self.Wd, self.dOut, self.dX, self.dWg, self.dWu, self.dWd, self.ws, _stream())
 
     def grads(self):
         return dict(dX=self.dX, dWg=self.dWg, dWu=self.dWu, dWd=self.dWd)
