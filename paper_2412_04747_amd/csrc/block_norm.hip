@@ -27,10 +27,12 @@ __device__ __forceinline__ void pack_cols(const float (&v)[V], int G, int64_t ro
     if (c % kHeldBlock == 0) scales[row * held_blocks(width) + c / kHeldBlock] = (uint8_t)b;
 }
 
-template <typename TA, typename TS, typename TO, int V, int NV, bool EVEN>
-__global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
+template <typename TA, typename TS, typename TO, typename S>
+__global__ __launch_bounds__(block_threads(S::GC)) void block_fwd_kernel(BlockFwdArgs a) {
+    constexpr int V = S::V, NV = S::NV;
+    constexpr bool EVEN = S::LIE == kEven;
     __shared__ float lds[4 * (kBlock / 64)];
-    const Shape sh(a.G);
+    const RowLanes<S> sh(a.G, a.width);
     const float inv = 1.f / (float)a.width;
     float w1[NV][V], w2[NV][V], gate[NV][V];
 #pragma unroll
@@ -46,10 +48,10 @@ __global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
     }
     int turn = 0;
     // (the trip count is the same for all threads of a workgroup whose rows are its own: the barrier in row_sums)
-    for (int64_t row0 = (int64_t)blockIdx.x * sh.rows_per_block; row0 < a.rows; row0 += (int64_t)gridDim.x * sh.rows_per_block) {
+    for (int64_t row0 = (int64_t)blockIdx.x * sh.rows(); row0 < a.rows; row0 += (int64_t)gridDim.x * sh.rows()) {
         const int64_t row = row0 + sh.group;
         const bool live = row < a.rows;
-        const int t = row_type(a.p, row, live);
+        const int t = sh.type(a.p, row0, a.rows);
         const int64_t base = row * a.width;
         float x[NV][V], s[NV][V];
 #pragma unroll
@@ -73,12 +75,12 @@ __global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
                 pack_cols<EVEN>(s[j], sh.G, row, c, a.width, there, a.s_codes, a.s_scales);
             }
         }
-        float none = 0.f, q1 = 1.f, k1 = 1.f;
+        float q1 = 1.f, k1 = 1.f;
         if (a.p.w1) {
             float sq = 0.f;
 #pragma unroll
             for (int j = 0; j < NV; ++j) sq += dot_cols<V>(x[j], x[j]);
-            row_sums(sq, none, sh.G, lds, turn++);
+            row_sum(sq, sh.G, lds, turn++);
             if (!(sq <= FLT_MAX)) {          // (all lanes of the row, and where the row is a workgroup's, all of it)
                 k1 = kScaleDown;
                 sq = 0.f;
@@ -86,7 +88,7 @@ __global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
                     for (int e = 0; e < V; ++e) sq += (x[j][e] * k1) * (x[j][e] * k1);
-                row_sums(sq, none, sh.G, lds, turn++);
+                row_sum(sq, sh.G, lds, turn++);
             }
             q1 = rsqrtf(sq * inv + a.eps * k1 * k1);
         }
@@ -100,7 +102,7 @@ __global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
             }
         float q2 = 1.f, k2 = 1.f;
         if (a.out) {
-            row_sums(sq, none, sh.G, lds, turn++);
+            row_sum(sq, sh.G, lds, turn++);
             if (!(sq <= FLT_MAX)) {
                 k2 = kScaleDown;
                 sq = 0.f;
@@ -108,7 +110,7 @@ __global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
                     for (int e = 0; e < V; ++e) sq += (s[j][e] * k2) * (s[j][e] * k2);
-                row_sums(sq, none, sh.G, lds, turn++);
+                row_sum(sq, sh.G, lds, turn++);
             }
             q2 = rsqrtf(sq * inv + a.eps * k2 * k2);
         }
@@ -131,9 +133,10 @@ __global__ __launch_bounds__(kBlock) void block_fwd_kernel(BlockFwdArgs a) {
 
 template <typename TA, typename TS, typename TO>
 rgnn_status_t launch_fwd(const rgnn_block_norm_desc_t* d, const JunctionPlan& p, const BlockFwdArgs& a, hipStream_t st) {
-    return block_with_vectors<sizeof(TA) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
+    return block_with_shape<sizeof(TA) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto shape) -> rgnn_status_t {
+        using S = decltype(shape);
         KernelTimer timer(st, "block_norm_fwd");
-        block_fwd_kernel<TA, TS, TO, V(), NV(), even()><<<(unsigned)std::min<int64_t>(kMaxBlocks, p.turns), kBlock, 0, st>>>(a);
+        block_fwd_kernel<TA, TS, TO, S><<<(unsigned)std::min<int64_t>(kMaxBlocks, p.turns), block_threads(S::GC), 0, st>>>(a);
         RGNN_CHECK_LAUNCH();
         return RGNN_OK;
     });

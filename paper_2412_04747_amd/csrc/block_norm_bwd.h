@@ -17,60 +17,87 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kMaxBlocks = 512;
-constexpr int kWaves = kBlock / 64;
-constexpr int kTail = kWaves;            // places behind a type's columns in the LDS: shares of dscale
+// Wavefronts that share a SIMD.  The registers of 4 columns per lane would allow five, of 8 three: with the next row's tensors on their way three are enough.
+constexpr int per_simd(int cols, int GC) { return GC == kBlock || cols > 8 ? 2 : 3; }
+constexpr size_t kLdsBytes = 160 * 1024;      // of a compute unit
+constexpr int kSumsLds = 4 * (kBlock / 64);
+constexpr int kTail = kBlock / 64;       // places behind a type's columns in the LDS: shares of dscale
 
-__host__ __device__ inline int place_len(int width) { return (width + 3) / 4 * 4 + kTail; }
-__host__ __device__ inline int part_len(int T, int width) { return (T + 1) * (width + 1); }
+// A type's place: its columns, filled up to whole vectors of four, then shares of dscale.  In a workgroup's partial rows the shares are one (of four).
+__host__ __device__ inline int columns4(int width) { return (width + 3) / 4 * 4; }
+__host__ __device__ inline int place_len(int width) { return columns4(width) + kTail; }
+__host__ __device__ inline int part_len(int width) { return columns4(width) + 4; }
 
-// The parameters' gradients of column c (or, c = width, of the types' scales) from total(t): G[t] for t < T, dw2 for t = T.
+// i / n for i below 2^16 and a positive n
+__device__ __forceinline__ int quotient(int i, int n) { return (int)(((float)i + 0.5f) * (1.f / (float)n)); }
+
+// The parameters' gradients of columns c0 .. c0 + n - 1 of the partial rows' sums, by all threads of a workgroup.  at(t, c - c0): the place in the LDS of G[t], for
+// t = T of dw2; the column behind the last vector holds dscale.
 template <typename F>
-__device__ __forceinline__ void finish(const BlockBwdArgs& a, int c, F total) {
+__device__ __forceinline__ void finish(const BlockBwdArgs& a, int c0, int n, int threads, F at) {
     const int T = a.p.T;
-    if (c == a.width) {
-        if (a.grads.scale)
-            for (int t = 0; t < T; ++t) a.grads.scale[t] = total(t) + (a.accumulate ? a.grads.scale[t] : 0.f);
-        return;
-    }
-    const float w = a.p.w1 ? a.p.w1[c] : 1.f;
-    float dw = 0.f;
-    for (int t = 0; t < T; ++t) {
-        const float g = total(t);
-        const int64_t at = (int64_t)t * a.width + c;
-        dw += (a.p.gate ? a.p.gate[at] : 1.f) * g;
-        if (a.grads.gate) a.grads.gate[at] = w * g + (a.accumulate ? a.grads.gate[at] : 0.f);
-    }
-    if (a.grads.w_after) a.grads.w_after[c] = dw + (a.accumulate ? a.grads.w_after[c] : 0.f);
-    if (a.grads.w_before) a.grads.w_before[c] = total(T) + (a.accumulate ? a.grads.w_before[c] : 0.f);
-}
-
-template <typename TA, typename TS, typename TO, int V, int NV, bool EVEN, bool HELD>
-__global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
-    extern __shared__ float lds[];           // row_sums' halves, then the places of the types
-    const Shape sh(a.G);
-    const float inv = 1.f / (float)a.width;
-    const int T = a.p.T, len = place_len(a.width), slots = a.G > 64 ? 1 : kWaves, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    float* const places = lds + 4 * kWaves;
-    float* const mine = places + (a.G > 64 ? 0 : wave * (T + 1) * len);
-    if (a.sums) {
-        for (int i = threadIdx.x; i < slots * (T + 1) * len; i += kBlock) places[i] = 0.f;
-        __syncthreads();
-    }
-    float w1[NV][V], w2[NV][V], gate[NV][V], dw2[NV][V], G[NV][V], dscale = 0.f, scale = a.p.scale ? a.p.scale[0] : 1.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (sh.lane + j * sh.G) * V;
-        zero_cols<V>(dw2[j]);
-        zero_cols<V>(G[j]);
-#pragma unroll
-        for (int e = 0; e < V; ++e) w1[j][e] = w2[j][e] = gate[j][e] = 1.f;
-        if (c < a.width) {
-            if (a.p.w1) load_v<EVEN>(a.p.w1, c, a.width, w1[j]);
-            if (a.p.w2) load_v<EVEN>(a.p.w2, c, a.width, w2[j]);
-            if (a.p.gate) load_v<EVEN>(a.p.gate, c, a.width, gate[j]);
+    auto give = [&](float* p, float v) { *p = a.accumulate ? v + *p : v; };
+    for (int i = threadIdx.x; i < (T + 1) * n; i += threads) {
+        const int t = quotient(i, n), c = c0 + i - t * n;
+        float& g = at(t, c - c0);
+        if (c >= a.width) {
+            if (c == columns4(a.width) && t < T && a.grads.scale) give(a.grads.scale + t, g);
+        } else if (t == T) {
+            if (a.grads.w_before) give(a.grads.w_before + c, g);
+        } else {
+            if (a.grads.gate) give(a.grads.gate + t * a.width + c, (a.p.w1 ? a.p.w1[c] : 1.f) * g);
+            if (a.p.gate) g *= a.p.gate[t * a.width + c];
         }
     }
+    if (!a.grads.w_after) return;
+    __syncthreads();
+    for (int k = threadIdx.x; k < n && c0 + k < a.width; k += threads) {
+        float v = 0.f;
+        for (int t = 0; t < T; ++t) v += at(t, k);
+        give(a.grads.w_after + c0 + k, v);
+    }
+}
+
+template <typename TA, typename TS, typename TO, typename S, bool HELD>
+__global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)) void block_bwd_kernel(BlockBwdArgs a) {
+    extern __shared__ float lds[];           // row_sums' halves, then the places of the types
+    constexpr int V = S::V, NV = S::NV, kThreads = block_threads(S::GC);
+    constexpr bool WIDE = S::GC == kBlock, AHEAD = V * NV <= 8, EVEN = S::LIE == kEven;
+    constexpr int kWaves = kThreads / 64, slots = WIDE ? 1 : kWaves;
+    const RowLanes<S> sh(a.G, a.width);
+    const float inv = 1.f / (float)a.width;
+    const int T = a.p.T, len = place_len(a.width), wave = threadIdx.x >> 6;
+    float* const places = lds + kSumsLds;
+    float* const mine = places + (WIDE ? 0 : wave * (T + 1) * len);
+    if (a.sums) {
+        for (int i = threadIdx.x; i < slots * (T + 1) * (len / 4); i += kThreads) reinterpret_cast<float4*>(places)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        __syncthreads();
+    }
+    // gw: gate w1 of the type at hand
+    float w2[NV][V], gw[NV][V], dw2[NV][V], G[NV][V], dscale = 0.f, scale = 1.f;
+    auto load_type = [&](int t) {
+        scale = a.p.scale ? a.p.scale[t] : 1.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (!sh.in(j)) continue;
+            float w[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) gw[j][e] = w[e] = 1.f;
+            if (a.p.gate) sh.shared(a.p.gate + (unsigned)(t * a.width), j, gw[j]);
+            if (a.p.w1) sh.shared(a.p.w1, j, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) gw[j][e] *= w[e];
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        zero_cols<V>(dw2[j]);
+        zero_cols<V>(G[j]);
+        zero_cols<V>(gw[j]);
+        zero_cols<V>(w2[j]);
+        if (a.p.w2 && sh.in(j)) sh.shared(a.p.w2, j, w2[j]);
+    }
+    load_type(0);
     // adds a lane's sums to place t of its wavefront (workgroup); the lanes with `who`, those of a row together
     auto give = [&](bool who, int t, float (&v)[NV][V], float& tail) {
         const float sum = lanes_sum(tail, min(sh.G, 64));
@@ -78,17 +105,16 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
         auto add = [&]() {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int c = (sh.lane + j * sh.G) * V;
-                if (c < a.width) {
+                if (sh.in(j)) {
                     float o[V];
-                    load_cols<V>(at + c, o);
+                    load_cols<V>(at + sh.col(j), o);
 #pragma unroll
                     for (int e = 0; e < V; ++e) o[e] += v[j][e];
-                    store_cols<V>(at + c, o);
+                    store_cols<V>(at + sh.col(j), o);
                 }
                 zero_cols<V>(v[j]);
             }
-            if ((sh.lane & 63) == 0) at[len - kTail + (sh.G > 64 ? wave : 0)] += sum;
+            if ((sh.lane & 63) == 0) at[len - kTail + (WIDE ? wave : 0)] += sum;
             tail = 0.f;
         };
         if (sh.G >= 64) {
@@ -98,60 +124,94 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
         const unsigned long long which = __ballot(who);
         for (int k = 0; k < 64; k += sh.G) {
             if (!((which >> k) & 1)) continue;
-            if ((lane & ~(sh.G - 1)) == k) add();
+            if ((threadIdx.x & 63 & ~(sh.G - 1)) == (unsigned)k) add();
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
     };
+    // A row's tensors as they lie in memory: the next row's are on their way while a row is worked on, and its type is known before.
+    RawCols<TA, V> xr[NV];
+    RawCols<TS, V> sr[NV], dsr[NV];
+    RawCols<TO, V> dyr[NV];
+    CodeWords<V> xc[NV], sc[NV];
+    unsigned xb[NV], sb[NV];
+    auto clear_words = [](auto& w) {
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof(w) / 4); ++k) w[k] = 0;
+    };
+    auto fetch = [&](int64_t row0, int t) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if constexpr (HELD) {
+                clear_words(xc[j]);
+                clear_words(sc[j]);
+                xb[j] = sb[j] = 0;
+            } else {
+                clear_words(xr[j]);
+                clear_words(sr[j]);
+            }
+            clear_words(dyr[j]);
+            clear_words(dsr[j]);
+            if (t < 0 || !sh.in(j)) continue;
+            if constexpr (HELD) {
+                sh.template fetch<int8_t>(a.a, row0, j, xc[j]);
+                sh.template fetch<int8_t>(a.s, row0, j, sc[j]);
+                xb[j] = sh.fetch_scale(a.a_scales, row0, j);
+                sb[j] = sh.fetch_scale(a.s_scales, row0, j);
+            } else {
+                sh.template fetch<TA>(a.a, row0, j, xr[j]);
+                sh.template fetch<TS>(a.s, row0, j, sr[j]);
+            }
+            if (a.dy) sh.template fetch<TO>(a.dy, row0, j, dyr[j]);
+            if (a.ds) sh.template fetch<TS>(a.ds, row0, j, dsr[j]);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * sh.rows();
     int turn = 0, type = a.p.types ? -1 : 0;
-    for (int64_t row0 = (int64_t)blockIdx.x * sh.rows_per_block; row0 < a.rows; row0 += (int64_t)gridDim.x * sh.rows_per_block) {
-        const int64_t row = row0 + sh.group;
-        const bool live = row < a.rows;
-        const int t = row_type(a.p, row, live);
-        const int64_t base = row * a.width;
+    int64_t row0 = (int64_t)blockIdx.x * sh.rows();
+    int t = sh.type(a.p, row0, a.rows), next = AHEAD ? sh.type(a.p, row0 + step, a.rows) : 0;
+    if constexpr (AHEAD) fetch(row0, t);
+    // (the trip count is the same for all threads of a workgroup whose rows are its own: the barrier in row_sums)
+    for (; row0 < a.rows; row0 += step) {
+        if constexpr (!AHEAD) fetch(row0, t);
         float x[NV][V], s[NV][V], dy[NV][V], dt[NV][V];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (sh.lane + j * sh.G) * V;
-            zero_cols<V>(x[j]);
-            zero_cols<V>(s[j]);
-            zero_cols<V>(dy[j]);
-            zero_cols<V>(dt[j]);
-            if (t >= 0 && c < a.width) {
-                if constexpr (HELD) {
-                    CodeWords<V> xw, sw;
-                    load_codes<EVEN, V>(static_cast<const int8_t*>(a.a) + base, c, a.width, xw);
-                    load_codes<EVEN, V>(static_cast<const int8_t*>(a.s) + base, c, a.width, sw);
-                    const int64_t b = row * held_blocks(a.width) + c / kHeldBlock;
-                    from_codes<V>(xw, held_step(a.a_scales[b]), x[j]);
-                    from_codes<V>(sw, held_step(a.s_scales[b]), s[j]);
-                } else {
-                    load_v<EVEN>(static_cast<const TA*>(a.a) + base, c, a.width, x[j]);
-                    load_v<EVEN>(static_cast<const TS*>(a.s) + base, c, a.width, s[j]);
-                }
-                if (a.dy) load_v<EVEN>(static_cast<const TO*>(a.dy) + base, c, a.width, dy[j]);
-                if (a.ds) load_v<EVEN>(static_cast<const TS*>(a.ds) + base, c, a.width, dt[j]);
+            if constexpr (HELD) {
+                sh.template align<int8_t>(j, xc[j]);
+                sh.template align<int8_t>(j, sc[j]);
+                from_codes<V>(xc[j], held_step(xb[j]), x[j]);
+                from_codes<V>(sc[j], held_step(sb[j]), s[j]);
+            } else {
+                sh.template values<TA>(j, xr[j], x[j]);
+                sh.template values<TS>(j, sr[j], s[j]);
             }
+            sh.template values<TO>(j, dyr[j], dy[j]);
+            sh.template values<TS>(j, dsr[j], dt[j]);
         }
-        const bool change = t >= 0 && t != type;
+        const int now = t;
+        const bool live = row0 + sh.group < a.rows;
+        if constexpr (AHEAD) {
+            t = next;
+            fetch(row0 + step, t);
+            next = sh.type(a.p, row0 + 2 * step, a.rows);
+        } else {
+            t = sh.type(a.p, row0 + step, a.rows);
+        }
+        const bool change = now >= 0 && now != type;
         if (__any(change)) {
             if (a.sums) give(change && type >= 0, max(type, 0), G, dscale);
             if (change) {
-                type = t;
-                scale = a.p.scale ? a.p.scale[t] : 1.f;
-#pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    const int c = (sh.lane + j * sh.G) * V;
-                    if (a.p.gate && c < a.width) load_v<EVEN>(a.p.gate + (int64_t)t * a.width, c, a.width, gate[j]);
-                }
+                type = now;
+                load_type(now);
             }
         }
-        float none = 0.f, q1 = 1.f, k1 = 1.f;
+        float q1 = 1.f, k1 = 1.f;
         if (a.p.w1) {
             float sq = 0.f;
 #pragma unroll
             for (int j = 0; j < NV; ++j) sq += dot_cols<V>(x[j], x[j]);
-            row_sums(sq, none, sh.G, lds, turn++);
+            row_sum(sq, sh.G, lds, turn++);
             if (!(sq <= FLT_MAX)) {          // as in the forward; the scaled values take their place
                 k1 = kScaleDown;
                 sq = 0.f;
@@ -162,7 +222,7 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
                         x[j][e] *= k1;
                         sq += x[j][e] * x[j][e];
                     }
-                row_sums(sq, none, sh.G, lds, turn++);
+                row_sum(sq, sh.G, lds, turn++);
             }
             q1 = rsqrtf(sq * inv + a.eps * k1 * k1);
         }
@@ -172,7 +232,7 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    u[j][e] = scale * s[j][e] + gate[j][e] * (x[j][e] * q1 * w1[j][e]);
+                    u[j][e] = scale * s[j][e] + x[j][e] * q1 * gw[j][e];
                     sq += u[j][e] * u[j][e];
                     gs += dy[j][e] * w2[j][e] * u[j][e];
                 }
@@ -191,9 +251,9 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
                     }
                 row_sums(sq, gs, sh.G, lds, turn++);
             }
-            // (with v = k u: q(u) = k q(v), u q(u)^2 mean(g u) = v q(v)^2 mean(g v))
+            // (with v = k u: q(u) = k q(v), u q(u)^2 mean(g u) = v q(v)^2 mean(g v); a row that stands for nothing has zeros here, with eps = 0 NaN)
             const float q2 = rsqrtf(sq * inv + a.eps * k2 * k2), along = q2 * q2 * (gs * inv), qk = q2 * k2;
-            if (t >= 0) {
+            if (now >= 0) {
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -209,29 +269,34 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int e = 0; e < V; ++e) ha += dt[j][e] * gate[j][e] * w1[j][e] * x[j][e];
-            row_sums(ha, none, sh.G, lds, turn++);
+                for (int e = 0; e < V; ++e) ha += dt[j][e] * gw[j][e] * x[j][e];
+            row_sum(ha, sh.G, lds, turn++);
             along = q1 * q1 * (ha * inv);
         }
+        if (!live || (now < 0 && a.accumulate)) continue;
         const float qk = q1 * k1;
+        TA* const da_row = sh.template row<TA>(a.da, row0);
+        TS* const ds_row = sh.template row<TS>(a.dstream, row0);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (sh.lane + j * sh.G) * V;
-            if (live && c < a.width && (t >= 0 || !a.accumulate)) {
-                float da[V], dstream[V];
+            if (!sh.in(j)) continue;
+            float da[V], dstream[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                da[e] = now >= 0 ? qk * (dt[j][e] * gw[j][e] - x[j][e] * along) : 0.f;
+                dstream[e] = scale * dt[j][e];
+            }
+            if (now >= 0) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float h = dt[j][e] * gate[j][e] * w1[j][e];
-                    da[e] = t >= 0 ? qk * (h - x[j][e] * along) : 0.f;
-                    dstream[e] = t >= 0 ? scale * dt[j][e] : 0.f;
-                    if (t >= 0) {
-                        G[j][e] += dt[j][e] * (x[j][e] * q1);
-                        dscale += dt[j][e] * s[j][e];
-                    }
+                    G[j][e] += dt[j][e] * (x[j][e] * q1);
+                    dscale += dt[j][e] * s[j][e];
                 }
-                if (a.da) put<EVEN>(static_cast<TA*>(a.da) + base, c, a.width, da, a.accumulate);
-                if (a.dstream) put<EVEN>(static_cast<TS*>(a.dstream) + base, c, a.width, dstream, a.accumulate);
+            } else {
+                zero_cols<V>(dstream);
             }
+            if (a.da) put<EVEN>(da_row, sh.col(j), a.width, da, a.accumulate);
+            if (a.dstream) put<EVEN>(ds_row, sh.col(j), a.width, dstream, a.accumulate);
         }
     }
     if (!a.sums) return;
@@ -239,41 +304,48 @@ __global__ __launch_bounds__(kBlock) void block_bwd_kernel(BlockBwdArgs a) {
     float unused = 0.f;
     give(true, T, dw2, unused);
     __syncthreads();
-    for (int i = threadIdx.x; i < part_len(T, a.width); i += kBlock) {
-        const int t = i / (a.width + 1), c = i - t * (a.width + 1);
-        float v = 0.f;
+    // the wavefronts' places in order
+    const int L4 = part_len(a.width) / 4;
+    for (int i = threadIdx.x; i < (T + 1) * L4; i += kThreads) {
+        const int t = quotient(i, L4), c = 4 * (i - t * L4);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto add = [&](const float4& o) { v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w; };
         for (int k = 0; k < slots; ++k) {
-            const float* const at = places + (k * (T + 1) + t) * len;
-            if (c < a.width) {
-                v += at[c];
-            } else {
-#pragma unroll
-                for (int q = 0; q < kTail; ++q) v += at[len - kTail + q];
-            }
+            const float4* const at = reinterpret_cast<const float4*>(places + (k * (T + 1) + t) * len + c);
+            add(at[0]);
+            if (c == L4 * 4 - 4) add(at[1]);
         }
-        if (gridDim.x > 1) a.part[(int64_t)blockIdx.x * part_len(T, a.width) + i] = v;
-        else places[t * len + (c < a.width ? c : len - kTail)] = v;          // (no other lane reads these)
+        if (c == L4 * 4 - 4) v = make_float4(v.x + v.y + v.z + v.w, 0.f, 0.f, 0.f);
+        // (what another lane reads is in no lane's way: a place's vectors are read here by this lane alone)
+        *reinterpret_cast<float4*>(gridDim.x > 1 ? a.part + ((int64_t)blockIdx.x * (T + 1) + t) * part_len(a.width) + c : places + t * len + c) = v;
     }
     if (gridDim.x > 1) return;
     __syncthreads();
-    for (int c = threadIdx.x; c <= a.width; c += kBlock) finish(a, c, [&](int t) { return places[t * len + (c < a.width ? c : len - kTail)]; });
+    finish(a, 0, part_len(a.width), kThreads, [&](int t, int c) -> float& { return places[t * len + c]; });
 }
 
-// (what two turns of a workgroup finish is left to one: the sums then need no second launch)
+inline size_t lds_bytes(const rgnn_block_norm_desc_t* d, const JunctionPlan& p, bool sums) {
+    // (places of types * (width + 12) <= 4096, four of them at most: 82 KB)
+    return sizeof(float) * (kSumsLds + (sums ? (size_t)(p.G == kBlock ? 1 : block_threads(p.G) / 64) * (d->types + 1) * place_len(d->width) : 0));
+}
+// As many as are resident at once, so that none comes in a second turn.  (What two turns of a workgroup finish is left to one: the sums then need no second launch.)
 inline int workgroups(const rgnn_block_norm_desc_t* d) {
     const JunctionPlan p = block_plan(d);
-    return p.turns <= 2 ? (int)std::min<int64_t>(p.turns, 1) : (int)std::min<int64_t>(kMaxBlocks, p.turns);
+    if (p.turns <= 2) return (int)std::min<int64_t>(p.turns, 1);
+    const int waves = 4 * per_simd(p.V * p.NV, p.G) / (block_threads(p.G) / 64), room = (int)(kLdsBytes / lds_bytes(d, p, true));
+    const int64_t most = 256 * std::max(1, std::min(waves, room));
+    return (int)std::min(most, p.turns);
 }
 
 template <typename TA, typename TS, typename TO, bool HELD>
 rgnn_status_t launch_rows(const rgnn_block_norm_desc_t* d, const JunctionPlan& p, const BlockBwdArgs& a, hipStream_t st) {
-    return block_with_vectors<sizeof(TA) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto V, auto NV, auto even) -> rgnn_status_t {
-        auto* const kernel = block_bwd_kernel<TA, TS, TO, V(), NV(), even(), HELD>;
-        // (at most eight wavefronts' places of types * (width + 12) <= 4096: 160 KB)
-        const size_t lds = sizeof(float) * (4 * kWaves + (a.sums ? (size_t)(p.G > 64 ? 1 : kWaves) * (d->types + 1) * place_len(d->width) : 0));
+    return block_with_shape<sizeof(TA) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto shape) -> rgnn_status_t {
+        using S = decltype(shape);
+        auto* const kernel = block_bwd_kernel<TA, TS, TO, S, HELD>;
+        const size_t lds = lds_bytes(d, p, a.sums);
         RGNN_TRY(allow_dynamic_lds(reinterpret_cast<const void*>(kernel), lds));
         KernelTimer timer(st, "block_norm_bwd");
-        kernel<<<workgroups(d), kBlock, lds, st>>>(a);
+        kernel<<<workgroups(d), block_threads(S::GC), lds, st>>>(a);
         RGNN_CHECK_LAUNCH();
         return RGNN_OK;
     });

@@ -28,6 +28,7 @@ constexpr int kDppQuadSwap1 = 0xB1;      // quad_perm:[1,0,3,2]
 constexpr int kDppQuadSwap2 = 0x4E;      // quad_perm:[2,3,0,1]
 constexpr int kDppHalfMirror = 0x141;    // lane i <-> 7 - i within each 8 lanes
 constexpr int kDppMirror = 0x140;        // lane i <-> 15 - i within each 16 lanes
+constexpr int kDppRowRotate = 0x120;     // + n: lane i <- (i + n) % 16 or (i - n) % 16 of each 16 lanes
 constexpr int kDppRowBcast0 = 0x150;     // + n: every lane of a row reads the row's lane n
 
 // sum over an aligned group of W lanes (W a power of two, at most 64); every lane of the group gets the
@@ -86,6 +87,16 @@ __device__ __forceinline__ Tv group_lane(Tv v, int lane) {
     }
     return __shfl(v, lane, W);
 }
+// A lane's value and those 16 and 32 lanes further, added up as two exchanges would, on the VALU.
+__device__ __forceinline__ float half_rows_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halves_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float rows_sum(float v) { return halves_sum(half_rows_sum(v)); }
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));

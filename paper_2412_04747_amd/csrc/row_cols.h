@@ -40,14 +40,42 @@ __device__ __forceinline__ void store_v(T* row, int c, int width, const float (&
     }
 }
 
+// V elements as they lie in memory, for rows that are on their way while others are worked on.
+template <typename T, int V> using RawCols = unsigned[V * sizeof(T) / 4];
+template <typename T, int V>
+__device__ __forceinline__ void raw_values(const RawCols<T, V>& w, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        v[e] = __uint_as_float(sizeof(T) == 4 ? w[e * sizeof(T) / 4] : e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+}
+// Moves words down by `bytes`, zeros after them.
+template <int N>
+__device__ __forceinline__ void move_down(unsigned (&w)[N], int bytes) {
+    if constexpr (N == 1) {
+        w[0] >>= 8 * bytes;
+    } else if constexpr (N == 2) {
+        const unsigned long long v = ((unsigned long long)w[1] << 32 | w[0]) >> (8 * bytes);
+        w[0] = (unsigned)v;
+        w[1] = (unsigned)(v >> 32);
+    } else {
+#pragma unroll
+        for (int k = 1; k < N; k *= 2)       // (whole words: fp32)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const unsigned here = w[i], there = i + k < N ? w[i + k < N ? i + k : 0] : 0u;       // (values: a choice between places would put w into memory)
+                w[i] = bytes & (4 * k) ? there : here;
+            }
+    }
+}
+
 // Sum over the G lanes of a row (G a power of two up to 64), or over the workgroup.
 __device__ __forceinline__ float lanes_sum(float v, int G) {
     if (G >= 2) v += dpp_move<kDppQuadSwap1>(v);
     if (G >= 4) v += dpp_move<kDppQuadSwap2>(v);
     if (G >= 8) v += dpp_move<kDppHalfMirror>(v);
     if (G >= 16) v += dpp_move<kDppMirror>(v);
-    if (G >= 32) v += __shfl_xor(v, 16);
-    if (G >= 64) v += __shfl_xor(v, 32);
+    if (G >= 32) v = half_rows_sum(v);
+    if (G >= 64) v = halves_sum(v);
     return v;
 }
 
@@ -76,6 +104,19 @@ __device__ __forceinline__ void row_sums(float& a, float& b, int G, float* lds, 
         a += at[i];
         b += at[W + i];
     }
+}
+
+// One sum.
+__device__ __forceinline__ void row_sum(float& a, int G, float* lds, int turn) {
+    a = lanes_sum(a, min(G, 64));
+    if (G <= 64) return;
+    constexpr int W = kBlock / 64;
+    float* const at = lds + (turn & 1) * 2 * W;
+    if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) a += at[i];
 }
 
 // What a row's values are multiplied by where their squares' sum is infinite.  Any finite row's sum is in range then, 2^-32 or more, and the squares
