@@ -19,6 +19,7 @@ struct BlockParams {
 struct BlockFwdArgs {
     int64_t rows;
     int width, G;
+    int streaming;           // sum and out are more than the caches hold
     float eps;
     BlockParams p;
     const void* a; const void* s;
@@ -29,6 +30,7 @@ struct BlockFwdArgs {
 struct BlockBwdArgs {
     int64_t rows;
     int width, G, accumulate;
+    int streaming;           // dA and dS are more than the caches hold, and nothing is added to them
     float eps;
     BlockParams p;
     const void* a; const void* s;        // codes, where they are held in 8 bits
@@ -98,6 +100,15 @@ rgnn_status_t block_with_types(const rgnn_block_norm_desc_t* d, F f) {
     return d->a_dtype == RGNN_BF16 ? second(b16) : second(f32);
 }
 
+// N words at an address that is a multiple of A.
+template <int N, int A> struct Words;
+template <> struct Words<1, 1> { typedef unsigned type __attribute__((aligned(1))); };
+template <> struct Words<1, 4> { typedef unsigned type; };
+template <> struct Words<2, 2> { typedef unsigned type __attribute__((ext_vector_type(2), aligned(2))); };
+template <> struct Words<2, 8> { typedef unsigned type __attribute__((ext_vector_type(2))); };
+template <> struct Words<4, 4> { typedef unsigned type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct Words<4, 16> { typedef unsigned type __attribute__((ext_vector_type(4))); };
+
 // The lanes of a workgroup over its rows: G of them share a row, vector j of a lane begins at column col(j).  A tensor's address is that of the workgroup's
 // first row, the same for all lanes, and an offset of 32 bits that does not change from row to row.  A short vector is read from `width - V` on and moved down by what it
 // overlaps, so that its lane takes no way of its own (which would wait for each load by itself).
@@ -129,7 +140,9 @@ struct RowLanes {
                 else w[e / 4] |= (unsigned)reinterpret_cast<const uint8_t*>(p)[e] << (8 * (e & 3));
             }
         } else {
-            __builtin_memcpy(w, even ? static_cast<const char*>(__builtin_assume_aligned(p, bytes < 16 ? bytes : 16)) : p, bytes);
+            // (with the hint that no line is read again)
+            const auto t = __builtin_nontemporal_load(reinterpret_cast<const typename Words<N, even ? bytes : (int)sizeof(T)>::type*>(p));
+            __builtin_memcpy(w, &t, bytes);
         }
     }
     // Vector j of the lane's row as it lies in memory, and what is left to do with it.
@@ -145,9 +158,15 @@ struct RowLanes {
     }
     // vector j of a row of fp32 that all rows share
     __device__ __forceinline__ void shared(const float* p, int j, float (&v)[V]) const {
-        RawCols<float, V> w;
-        words<float>(reinterpret_cast<const char*>(p + from(j)), j, w);
-        values<float>(j, w, v);
+        if constexpr (even) {
+            load_cols<V>(p + col(j), v);
+        } else if constexpr (S::LIE == kUneven) {
+            RawCols<float, V> w;
+            __builtin_memcpy(w, p + from(j), sizeof(w));
+            values<float>(j, w, v);
+        } else {
+            load_v<false>(p, col(j), width, v);
+        }
     }
     __device__ __forceinline__ unsigned fetch_scale(const uint8_t* scales, int64_t row0, int j) const {
         const int nb = held_blocks(width);

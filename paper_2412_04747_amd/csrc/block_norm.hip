@@ -13,18 +13,26 @@ namespace rgnn {
 
 namespace {
 
-constexpr int kMaxBlocks = 1024;
+// Workgroups of four wavefronts (of whole rows: eight): with the next row's tensors on their way, four to a compute unit are enough for 4 columns per lane, three for more.  In us,
+// with 512 / 768 / 1024 / 1536:  1M rows of 64, fp32: 181 / 177 / 179 / 192; 500000 of mixed types: 101 / 97 / 89 / 90; 200017 of 128 left in 8 bits: 93 / 84 / 80 / 81
+//                                2M rows of 128, bf16: 357 / 365 / 377 / 404; 500000: 90 / 87 / 88 / 94; 200000 rows of 349, fp32: 226 / 238 / 256 / 258
+constexpr int most_blocks(int cols, int GC) { return cols <= 4 || GC == kBlock ? 1024 : 768; }
 constexpr int kMaxWidth = 8192;
+// What is left for the next kernel in the 256 MB of the last cache: results past that are stored with the hint that they are not read from there (1M rows of 64, fp32, 512 MB of
+// gradients: 304 us without the hints of loads and stores, 285 with; 2M rows of 128 in bf16, from 8 bits: 510 and 484).
+constexpr size_t kCachedBytes = 192u << 20;
 
-// Codes and scales of a row's columns c .. c + V - 1, by all lanes of the row (`there`: of its tensor too); G lanes have the row.
-template <bool EVEN, int V>
-__device__ __forceinline__ void pack_cols(const float (&v)[V], int G, int64_t row, int c, int width, bool there, int8_t* codes, uint8_t* scales) {
-    const unsigned b = scale_byte(lanes_max(bits_max(v), min(G, kHeldBlock / V)));
+// Codes and scales of vector j of a row, by all its lanes; live: the row is one of the tensor's.
+template <typename S>
+__device__ __forceinline__ void pack_cols(const RowLanes<S>& sh, const float (&v)[S::V], int64_t row0, int j, bool live, int8_t* codes, uint8_t* scales) {
+    constexpr int V = S::V;
+    const unsigned b = scale_byte(lanes_max(bits_max(v), min(sh.G, kHeldBlock / V)));
     CodeWords<V> w;
     to_codes(v, b, w);
-    if (!there) return;
-    store_codes<EVEN, V>(codes + row * width, c, width, w);
-    if (c % kHeldBlock == 0) scales[row * held_blocks(width) + c / kHeldBlock] = (uint8_t)b;
+    if (!live || !sh.in(j)) return;
+    const int c = sh.col(j), nb = held_blocks(sh.width);
+    store_codes<S::LIE == kEven, V>(sh.template row<int8_t>(codes, row0), c, sh.width, w);
+    if (c % kHeldBlock == 0) (scales + row0 * nb)[(unsigned)(sh.group * nb + c / kHeldBlock)] = (uint8_t)b;
 }
 
 template <typename TA, typename TS, typename TO, typename S>
@@ -33,46 +41,74 @@ __global__ __launch_bounds__(block_threads(S::GC)) void block_fwd_kernel(BlockFw
     constexpr bool EVEN = S::LIE == kEven;
     __shared__ float lds[4 * (kBlock / 64)];
     const RowLanes<S> sh(a.G, a.width);
+    constexpr bool AHEAD = V * NV <= 8;
     const float inv = 1.f / (float)a.width;
-    float w1[NV][V], w2[NV][V], gate[NV][V];
+    // gw: gate w1 of the type at hand
+    float w2[NV][V], gw[NV][V], scale = 1.f;
+    auto load_type = [&](int t) {
+        scale = a.p.scale ? a.p.scale[t] : 1.f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (!sh.in(j)) continue;
+            float w[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) gw[j][e] = w[e] = 1.f;
+            if (a.p.gate) sh.shared(a.p.gate + (unsigned)(t * a.width), j, gw[j]);
+            if (a.p.w1) sh.shared(a.p.w1, j, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) gw[j][e] *= w[e];
+        }
+    };
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-        const int c = (sh.lane + j * sh.G) * V;
-#pragma unroll
-        for (int e = 0; e < V; ++e) w1[j][e] = w2[j][e] = gate[j][e] = 1.f;
-        if (c < a.width) {
-            if (a.p.w1) load_v<EVEN>(a.p.w1, c, a.width, w1[j]);
-            if (a.p.w2) load_v<EVEN>(a.p.w2, c, a.width, w2[j]);
-            if (a.p.gate && !a.p.types) load_v<EVEN>(a.p.gate, c, a.width, gate[j]);
-        }
+        zero_cols<V>(gw[j]);
+        zero_cols<V>(w2[j]);
+        if (a.p.w2 && sh.in(j)) sh.shared(a.p.w2, j, w2[j]);
     }
-    int turn = 0;
-    // (the trip count is the same for all threads of a workgroup whose rows are its own: the barrier in row_sums)
-    for (int64_t row0 = (int64_t)blockIdx.x * sh.rows(); row0 < a.rows; row0 += (int64_t)gridDim.x * sh.rows()) {
-        const int64_t row = row0 + sh.group;
-        const bool live = row < a.rows;
-        const int t = sh.type(a.p, row0, a.rows);
-        const int64_t base = row * a.width;
+    load_type(0);
+    // A row's tensors as they lie in memory: the next row's are on their way while a row is worked on, and its type is known before.
+    RawCols<TA, V> xr[NV];
+    RawCols<TS, V> sr[NV];
+    auto fetch = [&](int64_t row0, int t) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(xr[j]) / 4); ++k) xr[j][k] = 0;
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(sr[j]) / 4); ++k) sr[j][k] = 0;
+            if (t < 0 || !sh.in(j)) continue;
+            sh.template fetch<TA>(a.a, row0, j, xr[j]);
+            sh.template fetch<TS>(a.s, row0, j, sr[j]);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * sh.rows();
+    int turn = 0, type = 0;
+    int64_t row0 = (int64_t)blockIdx.x * sh.rows();
+    int now = sh.type(a.p, row0, a.rows), next = sh.type(a.p, row0 + step, a.rows);
+    if constexpr (AHEAD) fetch(row0, now);
+    // (the trip count is the same for all threads of a workgroup whose rows are its own: the barrier in row_sum)
+    for (; row0 < a.rows; row0 += step) {
+        const int t = now;
+        const bool live = row0 + sh.group < a.rows;
+        if constexpr (!AHEAD) fetch(row0, t);
         float x[NV][V], s[NV][V];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (sh.lane + j * sh.G) * V;
-            zero_cols<V>(x[j]);
-            zero_cols<V>(s[j]);
-            if (t >= 0 && c < a.width) {
-                load_v<EVEN>(static_cast<const TA*>(a.a) + base, c, a.width, x[j]);
-                load_v<EVEN>(static_cast<const TS*>(a.s) + base, c, a.width, s[j]);
-                if (a.p.gate && a.p.types) load_v<EVEN>(a.p.gate + (int64_t)t * a.width, c, a.width, gate[j]);
-            }
+            sh.template values<TA>(j, xr[j], x[j]);
+            sh.template values<TS>(j, sr[j], s[j]);
         }
-        const float scale = a.p.scale && t >= 0 ? a.p.scale[t] : 1.f;
+        now = next;
+        if constexpr (AHEAD) fetch(row0 + step, now);
+        next = sh.type(a.p, row0 + 2 * step, a.rows);
+        if (t >= 0 && t != type) {
+            type = t;
+            load_type(t);
+        }
         if (a.a_codes) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                const int c = (sh.lane + j * sh.G) * V;
-                const bool there = live && c < a.width;
-                pack_cols<EVEN>(x[j], sh.G, row, c, a.width, there, a.a_codes, a.a_scales);
-                pack_cols<EVEN>(s[j], sh.G, row, c, a.width, there, a.s_codes, a.s_scales);
+                pack_cols(sh, x[j], row0, j, live, a.a_codes, a.a_scales);
+                pack_cols(sh, s[j], row0, j, live, a.s_codes, a.s_scales);
             }
         }
         float q1 = 1.f, k1 = 1.f;
@@ -97,7 +133,7 @@ __global__ __launch_bounds__(block_threads(S::GC)) void block_fwd_kernel(BlockFw
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                s[j][e] = scale * s[j][e] + gate[j][e] * (x[j][e] * k1 * q1 * w1[j][e]);
+                s[j][e] = scale * s[j][e] + x[j][e] * k1 * q1 * gw[j][e];
                 sq += s[j][e] * s[j][e];
             }
         float q2 = 1.f, k2 = 1.f;
@@ -114,19 +150,24 @@ __global__ __launch_bounds__(block_threads(S::GC)) void block_fwd_kernel(BlockFw
             }
             q2 = rsqrtf(sq * inv + a.eps * k2 * k2);
         }
+        TS* const sum_row = sh.template row<TS>(a.sum, row0);
+        TO* const out_row = sh.template row<TO>(a.out, row0);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (sh.lane + j * sh.G) * V;
-            if (live && c < a.width) {
-                float y[V];
+            if (!live || !sh.in(j)) continue;
+            float y[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    s[j][e] = t >= 0 ? s[j][e] : 0.f;
-                    y[e] = t >= 0 ? s[j][e] * q2 * k2 * w2[j][e] : 0.f;
-                }
-                if (a.sum) store_v<EVEN>(static_cast<TS*>(a.sum) + base, c, a.width, s[j]);
-                if (a.out) store_v<EVEN>(static_cast<TO*>(a.out) + base, c, a.width, y);
+            for (int e = 0; e < V; ++e) {
+                s[j][e] = t >= 0 ? s[j][e] : 0.f;
+                y[e] = t >= 0 ? s[j][e] * q2 * k2 * w2[j][e] : 0.f;
             }
+            auto out = [&](auto* to, const float (&v)[V]) {
+                if constexpr (EVEN)
+                    if (a.streaming) return store_cols_nt<V>(to + sh.col(j), v);
+                store_v<EVEN>(to, sh.col(j), a.width, v);
+            };
+            if (a.sum) out(sum_row, s[j]);
+            if (a.out) out(out_row, y);
         }
     }
 }
@@ -136,7 +177,7 @@ rgnn_status_t launch_fwd(const rgnn_block_norm_desc_t* d, const JunctionPlan& p,
     return block_with_shape<sizeof(TA) + sizeof(TS) + sizeof(TO) == 6>(d, p, [&](auto shape) -> rgnn_status_t {
         using S = decltype(shape);
         KernelTimer timer(st, "block_norm_fwd");
-        block_fwd_kernel<TA, TS, TO, S><<<(unsigned)std::min<int64_t>(kMaxBlocks, p.turns), block_threads(S::GC), 0, st>>>(a);
+        block_fwd_kernel<TA, TS, TO, S><<<(unsigned)std::min<int64_t>(most_blocks(S::V * S::NV, S::GC), p.turns), block_threads(S::GC), 0, st>>>(a);
         RGNN_CHECK_LAUNCH();
         return RGNN_OK;
     });
@@ -223,7 +264,7 @@ extern "C" rgnn_status_t rgnn_block_norm_fwd(const rgnn_block_norm_desc_t* desc,
             if (held[i].overlaps(held[j])) RGNN_FAIL(RGNN_EINVAL, "codes and scales of a8 and s8 overlap");
     }
     const JunctionPlan p = block_plan(desc);
-    BlockFwdArgs f{rows, width, p.G, desc->eps, device_params(desc, params), a, s, sum, out, nullptr, nullptr, nullptr, nullptr};
+    BlockFwdArgs f{rows, width, p.G, sums.bytes + outs.bytes > kCachedBytes, desc->eps, device_params(desc, params), a, s, sum, out, nullptr, nullptr, nullptr, nullptr};
     if (a8) f.a_codes = a8->codes, f.a_scales = a8->scales, f.s_codes = s8->codes, f.s_scales = s8->scales;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return block_with_types(desc, [&](auto ta, auto ts, auto to) { return launch_fwd<decltype(ta), decltype(ts), decltype(to)>(desc, p, f, st); });
@@ -277,7 +318,8 @@ extern "C" rgnn_status_t rgnn_block_norm_bwd(const rgnn_block_norm_desc_t* desc,
         for (int j = 0; j < i; ++j)
             if (small[i].overlaps(small[j])) RGNN_FAIL(RGNN_EINVAL, "two parameters' gradients, or one and the workspace, overlap");
     }
-    BlockBwdArgs b{desc->rows, desc->width, block_plan(desc).G, (desc->flags & RGNN_FLAG_ACCUMULATE) != 0, desc->eps, device_params(desc, params), a, s,
+    const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
+    BlockBwdArgs b{desc->rows, desc->width, block_plan(desc).G, accumulate, !accumulate && das.bytes + dss.bytes > kCachedBytes, desc->eps, device_params(desc, params), a, s,
                    nullptr, nullptr, dOut, dSum, dA, dS, sums, nullptr, g};
     if (held && desc->rows > 0) b.a = a8->codes, b.a_scales = a8->scales, b.s = s8->codes, b.s_scales = s8->scales;
     return block_bwd(desc, b, held, workspace, static_cast<hipStream_t>(stream));

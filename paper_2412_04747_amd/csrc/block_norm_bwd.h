@@ -295,8 +295,13 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
             } else {
                 zero_cols<V>(dstream);
             }
-            if (a.da) put<EVEN>(da_row, sh.col(j), a.width, da, a.accumulate);
-            if (a.dstream) put<EVEN>(ds_row, sh.col(j), a.width, dstream, a.accumulate);
+            auto out = [&](auto* to, const float (&v)[V]) {
+                if constexpr (EVEN)
+                    if (a.streaming) return store_cols_nt<V>(to + sh.col(j), v);
+                put<EVEN>(to, sh.col(j), a.width, v, a.accumulate);
+            };
+            if (a.da) out(da_row, da);
+            if (a.dstream) out(ds_row, dstream);
         }
     }
     if (!a.sums) return;

@@ -191,6 +191,23 @@ __device__ __forceinline__ void store_cols(bf16_t* __restrict__ p, const float (
         *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]));
     }
 }
+// the same with a non-temporal hint: rows that no cache holds until they are read
+template <int V>
+__device__ __forceinline__ void store_cols_nt(float* __restrict__ p, const float (&v)[V]) {
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+        const rgnn_v4f t = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        __builtin_nontemporal_store(t, reinterpret_cast<rgnn_v4f*>(p) + q);
+    }
+}
+template <int V>
+__device__ __forceinline__ void store_cols_nt(bf16_t* __restrict__ p, const float (&v)[V]) {
+    typedef unsigned words __attribute__((ext_vector_type(V / 2)));
+    words t;
+#pragma unroll
+    for (int q = 0; q < V / 2; ++q) t[q] = bf16_pack2(v[2 * q], v[2 * q + 1]);
+    __builtin_nontemporal_store(t, reinterpret_cast<words*>(p));
+}
 template <int V>
 __device__ __forceinline__ void zero_cols(float (&v)[V]) {
 #pragma unroll
