@@ -150,7 +150,7 @@ struct RowLanes {
         words<T>(static_cast<const char*>(base) + row0 * width * sizeof(T) + (unsigned)((group * width + from(j)) * (int)sizeof(T)), j, w);
     }
     template <typename T> __device__ __forceinline__ void align(int j, unsigned (&w)[V * sizeof(T) / 4]) const {
-        if constexpr (S::LIE == kUneven) move_down(w, (col(j) - from(j)) * (int)sizeof(T));
+        if constexpr (S::LIE == kUneven) move_down<sizeof(T)>(w, (col(j) - from(j)) * (int)sizeof(T));
     }
     template <typename T> __device__ __forceinline__ void values(int j, RawCols<T, V>& w, float (&v)[V]) const {
         align<T>(j, w);

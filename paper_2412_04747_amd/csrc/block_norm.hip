@@ -18,9 +18,6 @@ namespace {
 //                                2M rows of 128, bf16: 357 / 365 / 377 / 404; 500000: 90 / 87 / 88 / 94; 200000 rows of 349, fp32: 226 / 238 / 256 / 258
 constexpr int most_blocks(int cols, int GC) { return cols <= 4 || GC == kBlock ? 1024 : 768; }
 constexpr int kMaxWidth = 8192;
-// What is left for the next kernel in the 256 MB of the last cache: results past that are stored with the hint that they are not read from there (1M rows of 64, fp32, 512 MB of
-// gradients: 304 us without the hints of loads and stores, 285 with; 2M rows of 128 in bf16, from 8 bits: 510 and 484).
-constexpr size_t kCachedBytes = 192u << 20;
 
 // Codes and scales of vector j of a row, by all its lanes; live: the row is one of the tensor's.
 template <typename S>
@@ -264,7 +261,7 @@ extern "C" rgnn_status_t rgnn_block_norm_fwd(const rgnn_block_norm_desc_t* desc,
             if (held[i].overlaps(held[j])) RGNN_FAIL(RGNN_EINVAL, "codes and scales of a8 and s8 overlap");
     }
     const JunctionPlan p = block_plan(desc);
-    BlockFwdArgs f{rows, width, p.G, sums.bytes + outs.bytes > kCachedBytes, desc->eps, device_params(desc, params), a, s, sum, out, nullptr, nullptr, nullptr, nullptr};
+    BlockFwdArgs f{rows, width, p.G, (int64_t)(sums.bytes + outs.bytes) > kCachedBytes, desc->eps, device_params(desc, params), a, s, sum, out, nullptr, nullptr, nullptr, nullptr};
     if (a8) f.a_codes = a8->codes, f.a_scales = a8->scales, f.s_codes = s8->codes, f.s_scales = s8->scales;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return block_with_types(desc, [&](auto ta, auto ts, auto to) { return launch_fwd<decltype(ta), decltype(ts), decltype(to)>(desc, p, f, st); });
@@ -319,7 +316,7 @@ extern "C" rgnn_status_t rgnn_block_norm_bwd(const rgnn_block_norm_desc_t* desc,
             if (small[i].overlaps(small[j])) RGNN_FAIL(RGNN_EINVAL, "two parameters' gradients, or one and the workspace, overlap");
     }
     const int accumulate = (desc->flags & RGNN_FLAG_ACCUMULATE) != 0;
-    BlockBwdArgs b{desc->rows, desc->width, block_plan(desc).G, accumulate, !accumulate && das.bytes + dss.bytes > kCachedBytes, desc->eps, device_params(desc, params), a, s,
+    BlockBwdArgs b{desc->rows, desc->width, block_plan(desc).G, accumulate, !accumulate && (int64_t)(das.bytes + dss.bytes) > kCachedBytes, desc->eps, device_params(desc, params), a, s,
                    nullptr, nullptr, dOut, dSum, dA, dS, sums, nullptr, g};
     if (held && desc->rows > 0) b.a = a8->codes, b.a_scales = a8->scales, b.s = s8->codes, b.s_scales = s8->scales;
     return block_bwd(desc, b, held, workspace, static_cast<hipStream_t>(stream));

@@ -48,8 +48,8 @@ __device__ __forceinline__ void raw_values(const RawCols<T, V>& w, float (&v)[V]
     for (int e = 0; e < V; ++e)
         v[e] = __uint_as_float(sizeof(T) == 4 ? w[e * sizeof(T) / 4] : e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
 }
-// Moves words down by `bytes`, zeros after them.
-template <int N>
+// Moves the elements of SIZE bytes in words down by `bytes`, fewer than there are, zeros after them.
+template <int SIZE, int N>
 __device__ __forceinline__ void move_down(unsigned (&w)[N], int bytes) {
     if constexpr (N == 1) {
         w[0] >>= 8 * bytes;
@@ -58,13 +58,21 @@ __device__ __forceinline__ void move_down(unsigned (&w)[N], int bytes) {
         w[0] = (unsigned)v;
         w[1] = (unsigned)(v >> 32);
     } else {
+        static_assert(SIZE >= 2, "halves of words at least");
 #pragma unroll
-        for (int k = 1; k < N; k *= 2)       // (whole words: fp32)
+        for (int k = 1; k < N; k *= 2)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const unsigned here = w[i], there = i + k < N ? w[i + k < N ? i + k : 0] : 0u;       // (values: a choice between places would put w into memory)
                 w[i] = bytes & (4 * k) ? there : here;
             }
+        if constexpr (SIZE == 2) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const unsigned here = w[i], there = i + 1 < N ? w[i + 1 < N ? i + 1 : 0] : 0u;
+                w[i] = bytes & 2 ? here >> 16 | there << 16 : here;
+            }
+        }
     }
 }
 
