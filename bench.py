@@ -299,8 +299,9 @@ def train_step_bench(args):
     g = A.Graph(N, R, c["src"], c["dst"], c["rel"])
     torch.manual_seed(synth.SEED0)
     layers = [A.RgatConv(R, d, c["slope"]), A.RgatConv(R, d, c["slope"])]
-    norms = [A.ResidualNorm(d) for _ in range(5)] if args.block else []
-    ffns = [A.GatedFfn(d, args.block) for _ in range(2)] if args.block else []
+    join = (lambda: A.BlockNorm(d, held=args.held)) if args.post_norm else (lambda: A.ResidualNorm(d))
+    norms = [A.ResidualNorm(d), *(join() for _ in range(4))] if args.block else []
+    ffns = [A.GatedFfn(d, args.block, held=args.held) for _ in range(2)] if args.block else []
     params = [q for l in layers + norms + ffns for q in l.parameters()]
     X = torch.tensor(c["X"], dtype=torch.float32, device="cuda")
     rng = np.random.default_rng(synth.SEED0)
@@ -330,6 +331,7 @@ def train_step_bench(args):
     for _ in range(args.warmup):
         step()
     torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
     B.rgnn_profile_start()
     t0 = time.perf_counter()
     for _ in range(args.steps):
@@ -339,7 +341,7 @@ def train_step_bench(args):
     rep = B.rgnn_profile_stop()
     lib_ms = sum(ms for _, ms in rep.values()) / args.steps
     print(f"[bench] train step {dt * 1e3 / args.steps:.3f} ms, of which {lib_ms:.3f} ms in the library's kernels; "
-          f"last loss {loss.item():.4f}", file=sys.stderr, flush=True)
+          f"last loss {loss.item():.4f}; at most {torch.cuda.max_memory_allocated() / 2 ** 30:.2f} GiB allocated", file=sys.stderr, flush=True)
     print(json.dumps({
         "metric": "edges/sec for 2-layer RGAT training step (fwd + NLL loss + bwd + SGD)",
         "value": 2 * E * args.steps / dt, "unit": "edges/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup,
@@ -347,6 +349,8 @@ def train_step_bench(args):
         "dtype": "f32", "data": "synthetic",
         "config": {"workload": f"configs[{args.config - 1}] graph, two RGAT layers of width {d}, N={N}, R={R}, E={E}"
                                + (f", each in a residual block with a feed-forward block of hidden width {args.block}" if args.block else "")
+                               + (", norms after the blocks, gates and residual scales" if args.post_norm else "")
+                               + (", rows of the blocks held in 8 bits" if args.held else "")
                                + (f", gradients clipped to norm {args.clip_norm:g}" if args.clip_norm else "")
                                + "; value counts every edge once per layer"},
         "library_kernel_ms_per_step": lib_ms}))
@@ -382,6 +386,10 @@ def main():
                          "log-softmax + NLL loss on 10%% of the nodes, SGD update (RGAT workloads only)")
     ap.add_argument("--block", type=int, default=0, metavar="HIDDEN",
                     help="with --train: each layer in a pre-norm residual block, followed by a gated feed-forward block of that hidden width")
+    ap.add_argument("--post-norm", action="store_true",
+                    help="with --block: a norm after each block too, and a gate and residual scale where its output joins the stream")
+    ap.add_argument("--held", action="store_true",
+                    help="with --block: the rows that the feed-forward blocks (and with --post-norm the junctions) keep for the backward are held in 8 bits")
     ap.add_argument("--clip-norm", type=float, default=0.0, help="with --train: clip the global norm of the gradients before the update")
     args = ap.parse_args()
     if args.gpus != 1:
@@ -394,6 +402,8 @@ def main():
     from paper_2412_04747_amd.harness import Graph
 
     assert torch.cuda.is_available(), "bench.py needs a GPU"
+    if (args.post_norm or args.held) and not args.block:
+        sys.exit("bench.py --post-norm / --held: only with --train --block")
     if args.train:
         return train_step_bench(args)
     if args.block or args.clip_norm:

@@ -8,6 +8,9 @@ training of a two-layer model with a negative-log-likelihood loss).
 
 `residual_norm` and `gated_ffn` (`ResidualNorm`, `GatedFfn`) are what stands between the layers of a residual
 model; they take fp32 or bf16 rows and need no graph (the layers here are fp32 only; the C calls also take bf16 rows).
+`block_norm` (`BlockNorm`) joins a block's output to the residual stream: norm after the block, gate and residual scale by node type, norm
+before the next block.  With held=True, `block_norm` and `gated_ffn` keep their rows for the backward in 8 bits (`pack_rows` has the
+format) instead of the tensors themselves: results are the same, gradients are those of the held values.
 `clip_grad_norm_` bounds the global norm of a model's gradients before the optimiser's step.
 
 The workspace of a (layer kind, width, options) combination is allocated once per graph, kept on the
@@ -140,8 +143,12 @@ def _rows(*tensors):
     for t in tensors:
         if t is not None and (t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda or t.device != device):
             raise TypeError("rgnn row operators take fp32 or bf16 CUDA tensors on one device")
-    # (a contiguous slice may still start between 16-byte boundaries)
-    return [t if t is None else t.contiguous() if t.data_ptr() % 16 == 0 or not t.is_contiguous() else t.clone() for t in tensors]
+    return [t if t is None else _aligned(t) for t in tensors]
+
+
+def _aligned(t):
+    """The tensor, contiguous and from a 16-byte boundary on (a contiguous slice may start between two)."""
+    return t.contiguous() if t.data_ptr() % 16 == 0 or not t.is_contiguous() else t.clone()
 
 
 _CODES = {torch.float32: B.RGNN_F32, torch.bfloat16: B.RGNN_BF16}
@@ -194,9 +201,129 @@ class _ResidualNorm(torch.autograd.Function):
         return None, None, dX if need_x else None, (dX if same else dR) if need_r else None, dW
 
 
+def _pack(x):
+    """(codes, scales) of contiguous rows in 8 bits."""
+    width = x.shape[-1]
+    rows = x.numel() // width if width else 0
+    codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty(*x.shape[:-1], -(-width // 32), dtype=torch.uint8, device=x.device)
+    B.rgnn_rows8_pack(B.make_rows8_desc(rows, width, _code(x.dtype)), x, B.rows8(codes, scales), _stream())
+    return codes, scales
+
+
+@torch.no_grad()
+def pack_rows(x):
+    """Rows (the last dimension, up to 8192) in 8 bits: (codes, scales), int8 of x's shape and a uint8 for every 32 columns of a row.  A value stands
+    for codes * 2^(scales - 133), off by at most half a step, 2^(scales - 134); the step is the least power of two with which the largest of the 32
+    rounds to at most 127.  An infinity or NaN makes its 32 columns NaN."""
+    x, = _rows(x)
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"pack_rows: rows of one column at least are wanted, got {tuple(x.shape)}")
+    with torch.cuda.device(x.device):
+        return _pack(x)
+
+
+@torch.no_grad()
+def unpack_rows(codes, scales, dtype=torch.float32):
+    """The rows that `pack_rows` gave, exact in fp32 and in bf16."""
+    if codes.dtype != torch.int8 or scales.dtype != torch.uint8 or not codes.is_cuda or scales.device != codes.device:
+        raise TypeError("unpack_rows: codes are int8 and scales uint8, on one GPU")
+    if codes.dim() < 1 or codes.shape[-1] < 1 or scales.shape != (*codes.shape[:-1], -(-codes.shape[-1] // 32)):
+        raise ValueError(f"unpack_rows: scales {tuple(scales.shape)} do not fit codes {tuple(codes.shape)}")
+    code, width = _code(dtype), codes.shape[-1]
+    with torch.cuda.device(codes.device):
+        codes, scales = _aligned(codes), scales.contiguous()
+        x = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+        B.rgnn_rows8_unpack(B.make_rows8_desc(codes.numel() // width, width, code), B.rows8(codes, scales), x, _stream())
+    return x
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, eps, out_dtype, held, num_types, types, a, s, w_after, w_before, gate, scale):
+        ctx.set_materialize_grads(False)
+        a, s, types, w_after, w_before, gate, scale = (None if t is None else _aligned(t) for t in (a, s, types, w_after, w_before, gate, scale))
+        width = a.shape[-1]
+        with torch.cuda.device(a.device):
+            ctx.desc = B.make_block_norm_desc(a.numel() // width, width, _code(a.dtype), _code(s.dtype), _code(out_dtype), num_types, eps)
+            total = torch.empty_like(s)
+            out = torch.empty(a.shape, dtype=out_dtype, device=a.device) if w_before is not None else None
+            a8 = s8 = None
+            ctx.held = held and any(ctx.needs_input_grad)
+            if ctx.held:
+                kept = [torch.empty(*a.shape[:-1], n, dtype=t, device=a.device) for _ in "as" for n, t in ((width, torch.int8), (-(-width // 32), torch.uint8))]
+                a8, s8 = B.rows8(*kept[:2]), B.rows8(*kept[2:])
+            B.rgnn_block_norm_fwd(ctx.desc, B.block_norm_params(types, w_after, gate, scale, w_before), a, s, total, out, a8, s8, _stream())
+        ctx.types_of = a.dtype, s.dtype
+        ctx.save_for_backward(types, w_after, w_before, gate, scale, *(kept if ctx.held else (a, s)))
+        return (out, total) if out is not None else total
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *grads):
+        types, w_after, w_before, gate, scale, *kept = ctx.saved_tensors
+        dOut, dSum = grads if w_before is not None else (None, *grads)
+        if dOut is None and dSum is None:
+            return (None,) * 11
+        dOut, dSum = _rows(dOut, dSum)
+        device = kept[0].device
+        with torch.cuda.device(device):
+            need = ctx.needs_input_grad[5:]
+            shape = kept[0].shape
+            dA, dS = (torch.empty(shape, dtype=t, device=device) if n else None for n, t in zip(need, ctx.types_of))
+            dw = [torch.empty_like(t) if n else None for n, t in zip(need[2:], (w_after, w_before, gate, scale))]
+            g = B.block_norm_grads(dw[0], dw[2], dw[3], dw[1])
+            a8, s8 = (B.rows8(*kept[:2]), B.rows8(*kept[2:])) if ctx.held else (None, None)
+            a, s = (None, None) if ctx.held else kept
+            ws = _buf(B.rgnn_block_norm_workspace_bytes(ctx.desc)) if any(need[2:]) else None
+            B.rgnn_block_norm_bwd(ctx.desc, B.block_norm_params(types, w_after, gate, scale, w_before), a, s, a8, s8, dOut, dSum, dA, dS, g, ws, _stream())
+        return (None, None, None, None, None, dA, dS, *dw)
+
+
+def block_norm(a, s, w_after=None, w_before=None, gate=None, scale=None, types=None, eps=1e-6, out_dtype=None, held=False):
+    """Joins a block's output `a` to the residual stream `s`, over the last dimension:
+        n = a / sqrt(mean(a^2) + eps) * w_after;   sum = scale[t] * s + gate[t] * n;   out = sum / sqrt(mean(sum^2) + eps) * w_before
+    and returns (out, sum), or sum alone without w_before.  t = types (int32, a's shape without the last dimension); gate [width] or [types,
+    width], scale [] or [types]; w_after, w_before [width]; all fp32.  What is not given is left out: the norm after the block, the gate (1), the scale (1),
+    the norm before the next.  sum has s's type, out has out_dtype (fp32 or bf16; default: a's).  A row whose type is not one of the parameters' stands for
+    nothing (a batch's padding): it is not read, and its results and gradients are zeros.
+    HGT's skip connection: gate = sigmoid(p)[:, None].expand(-1, width), scale = 1 - sigmoid(p).
+    held: a and s are kept for the backward in 8 bits."""
+    if out_dtype is not None and out_dtype not in _CODES:
+        raise TypeError(f"block_norm: out_dtype is fp32 or bf16, not {out_dtype}")
+    for t in (a, s):
+        _code(t.dtype)
+    if a.dim() < 1 or a.shape[-1] < 1 or s.shape != a.shape:
+        raise ValueError(f"block_norm: rows of one shape are wanted, got {tuple(a.shape)} and {tuple(s.shape)}")
+    width, counts = a.shape[-1], set()
+    for name, t, dims in (("w_after", w_after, (1,)), ("w_before", w_before, (1,)), ("gate", gate, (1, 2)), ("scale", scale, (0, 1))):
+        if t is None:
+            continue
+        if t.dtype != torch.float32:
+            raise TypeError(f"block_norm: {name} is fp32, not {t.dtype}")
+        if t.dim() not in dims or (name != "scale" and t.shape[-1] != width) or t.numel() == 0:
+            raise ValueError(f"block_norm: {name} of shape {tuple(t.shape)} does not fit rows of {width}")
+        if name in ("gate", "scale"):
+            counts.add(t.numel() if name == "scale" else t.numel() // width)
+    if len(counts) > 1:
+        raise ValueError(f"block_norm: gate and scale are of {sorted(counts)} types")
+    num_types = counts.pop() if counts else 1
+    if types is None and num_types > 1:
+        raise ValueError(f"block_norm: parameters of {num_types} types, but no types of the rows")
+    if types is not None:
+        if types.dtype != torch.int32:
+            raise TypeError(f"block_norm: types are int32, not {types.dtype}")
+        if types.shape != a.shape[:-1]:
+            raise ValueError(f"block_norm: types of shape {tuple(types.shape)} for rows {tuple(a.shape)}")
+    for t in (a, s, w_after, w_before, gate, scale, types):
+        if t is not None and (not t.is_cuda or t.device != a.device):
+            raise TypeError("block_norm takes tensors on one GPU")
+    return _BlockNorm.apply(float(eps), out_dtype or a.dtype, bool(held), num_types, types, a, s, w_after, w_before, gate, scale)
+
+
 class _GatedFfn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, act, X, Wg, Wu, Wd):
+    def forward(ctx, act, held, X, Wg, Wu, Wd):
         X, Wg, Wu, Wd = _rows(X, Wg, Wu, Wd)
         if Wg.dim() != 2 or X.dim() < 1 or X.shape[-1] != Wg.shape[0] or Wu.shape != Wg.shape or Wd.shape != Wg.shape[::-1]:
             raise ValueError(f"gated_ffn: shapes {tuple(X.shape)}, {tuple(Wg.shape)}, {tuple(Wu.shape)}, {tuple(Wd.shape)} do not fit")
@@ -208,20 +335,25 @@ class _GatedFfn(torch.autograd.Function):
                                        {"silu": B.RGNN_ACT_SILU, "relu": B.RGNN_ACT_RELU}[act])
             out = torch.empty_like(X)
             B.rgnn_ffn_fwd(ctx.desc, X, Wg, Wu, Wd, out, _buf(B.rgnn_ffn_workspace_bytes(ctx.desc)[0]), _stream())
-        ctx.save_for_backward(X, Wg, Wu, Wd)
+            ctx.held = held and any(ctx.needs_input_grad)
+            ctx.save_for_backward(Wg, Wu, Wd, *(_pack(X) if ctx.held else (X,)))
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dOut):
-        X, Wg, Wu, Wd = ctx.saved_tensors
+        Wg, Wu, Wd, *kept = ctx.saved_tensors
         dOut, = _rows(dOut)
-        need_x, *need_w = ctx.needs_input_grad[1:]
-        with torch.cuda.device(X.device):
-            dX = torch.empty_like(X) if need_x else None
+        need_x, *need_w = ctx.needs_input_grad[2:]
+        with torch.cuda.device(dOut.device):
+            dX = torch.empty_like(dOut) if need_x else None
             g = [torch.empty_like(W) if any(need_w) else None for W in (Wg, Wu, Wd)]
-            B.rgnn_ffn_bwd(ctx.desc, X, Wg, Wu, Wd, dOut, dX, *g, _buf(B.rgnn_ffn_workspace_bytes(ctx.desc)[1]), _stream())
-        return (None, dX, *(t if n else None for t, n in zip(g, need_w)))
+            ws = _buf(B.rgnn_ffn_workspace_bytes(ctx.desc)[1])
+            if ctx.held:
+                B.rgnn_ffn_bwd_rows8(ctx.desc, B.rows8(*kept), Wg, Wu, Wd, dOut, dX, *g, ws, _stream())
+            else:
+                B.rgnn_ffn_bwd(ctx.desc, kept[0], Wg, Wu, Wd, dOut, dX, *g, ws, _stream())
+        return (None, None, dX, *(t if n else None for t, n in zip(g, need_w)))
 
 
 def residual_norm(x, weight, residual=None, eps=1e-6, out_dtype=None):
@@ -232,11 +364,12 @@ def residual_norm(x, weight, residual=None, eps=1e-6, out_dtype=None):
     return _ResidualNorm.apply(float(eps), out_dtype or x.dtype, x, residual, weight)
 
 
-def gated_ffn(X, Wg, Wu, Wd, act="silu"):
-    """Gated feed-forward block (act(X Wg) * (X Wu)) Wd over the last dimension; Wg, Wu [d, hidden], Wd [hidden, d], all of X's type."""
+def gated_ffn(X, Wg, Wu, Wd, act="silu", held=False):
+    """Gated feed-forward block (act(X Wg) * (X Wu)) Wd over the last dimension; Wg, Wu [d, hidden], Wd [hidden, d], all of X's type.
+    held: X is kept for the backward in 8 bits."""
     if act not in ("silu", "relu"):
         raise ValueError(f"gated_ffn: unknown activation {act!r}")
-    return _GatedFfn.apply(act, X, Wg, Wu, Wd)
+    return _GatedFfn.apply(act, bool(held), X, Wg, Wu, Wd)
 
 
 def _apart(t):
@@ -355,17 +488,33 @@ class ResidualNorm(torch.nn.Module):
         return residual_norm(x, self.weight, residual, self.eps, self.out_dtype)
 
 
-class GatedFfn(torch.nn.Module):
-    def __init__(self, width, hidden, act="silu", dtype=torch.float32):
+class BlockNorm(torch.nn.Module):
+    """`block_norm` with its parameters: out, s = norm(a, s, types).  gate, scale: their first values, the same for all types and columns; after, before: whether
+    there is a norm after the block and one before the next."""
+
+    def __init__(self, width, num_types=1, gate=1.0, scale=1.0, after=True, before=True, eps=1e-6, out_dtype=None, held=False):
         super().__init__()
-        self.act = act
+        self.eps, self.out_dtype, self.held = eps, out_dtype, held
+        p = lambda value, *shape: torch.nn.Parameter(torch.full(shape, float(value), device="cuda"))
+        self.weight_after = p(1, width) if after else None
+        self.weight_before = p(1, width) if before else None
+        self.gate, self.scale = p(gate, num_types, width), p(scale, num_types)
+
+    def forward(self, a, s, types=None):
+        return block_norm(a, s, self.weight_after, self.weight_before, self.gate, self.scale, types, self.eps, self.out_dtype, self.held)
+
+
+class GatedFfn(torch.nn.Module):
+    def __init__(self, width, hidden, act="silu", dtype=torch.float32, held=False):
+        super().__init__()
+        self.act, self.held = act, held
         p = lambda *shape, fan_in: torch.nn.Parameter(_param(*shape, fan_in=fan_in).detach().to(dtype))
         self.Wg, self.Wu = p(width, hidden, fan_in=width), p(width, hidden, fan_in=width)
         self.Wd = p(hidden, width, fan_in=hidden)
 
     def forward(self, X):
-        return gated_ffn(X, self.Wg, self.Wu, self.Wd, self.act)
+        return gated_ffn(X, self.Wg, self.Wu, self.Wd, self.act, self.held)
 
 
 __all__ = ["Graph", "rgat", "rgcn", "hgt", "RgatConv", "RgcnConv", "HgtConv", "release", "residual_norm", "gated_ffn",
-           "clip_grad_norm_", "ResidualNorm", "GatedFfn"]
+           "clip_grad_norm_", "ResidualNorm", "GatedFfn", "block_norm", "BlockNorm", "pack_rows", "unpack_rows"]

@@ -51,7 +51,7 @@ __device__ __forceinline__ void grad_block(const FfnGradArgs& k, int split, int 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & (MT - 1), kg = lane / MT;
     const FfnArgs& a = k.a;
     const int F = a.hidden, FP = a.chunks * kHid, h = (group * WAVES + wave) * MT + m;
-    const bool mine = (group * WAVES + wave) * MT < FP;
+    const bool mine = (group * WAVES + wave) * MT < F;       // (what a chunk's end leaves in `part` is read by nobody)
 
     bf16x8 wg[S][PL], wu[S][PL], wd[S][PL];
 #pragma unroll

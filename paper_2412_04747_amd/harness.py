@@ -255,6 +255,7 @@ class BlockNormLayer:
         self.desc = B.make_block_norm_desc(rows, width, ca, cs, co, types, eps, flags)
         self.ws = _buf(B.rgnn_block_norm_workspace_bytes(self.desc))
         e = lambda *shape, t=torch.float32: torch.empty(*shape, device="cuda", dtype=t)
+        self._table = B.block_norm_params()       # (filled in at each call)
         self.types = self.w_after = self.w_before = self.gate = self.scale = None
         self.a = self.s = self.dOut = self.dSum = None
         self.sum, self.out, self.dA, self.dS = e(rows, width, t=ts), e(rows, width, t=to), e(rows, width, t=ta), e(rows, width, t=ts)
@@ -262,7 +263,9 @@ class BlockNormLayer:
         self.held_a, self.held_s = (Rows8(rows, width), Rows8(rows, width)) if held else (None, None)
 
     def _params(self):
-        return B.block_norm_params(self.types, self.w_after, self.gate, self.scale, self.w_before)
+        p, at = self._table, B._addr
+        p.row_types, p.w_after, p.gate, p.scale, p.w_before = at(self.types), at(self.w_after), at(self.gate), at(self.scale), at(self.w_before)
+        return p
 
     def _held(self):
         return (None, None) if self.held_a is None else (self.held_a.tensors(), self.held_s.tensors())

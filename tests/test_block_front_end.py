@@ -1,0 +1,45 @@
+"""What the Python entry points of the junction and of rows in 8 bits refuse by themselves, before anything reaches the library (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2412_04747_amd import autograd as A
+from paper_2412_04747_amd import harness as H
+
+x, w = torch.zeros(6, 8), torch.ones(8)
+kinds = torch.zeros(6, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("kind,word,call", [
+    (TypeError, "out_dtype", lambda: A.block_norm(x, x, w, out_dtype=torch.float16)),
+    (TypeError, "fp32 or bf16", lambda: A.block_norm(x.half(), x.half(), w)),
+    (TypeError, "fp32 or bf16", lambda: A.block_norm(x, x.double(), w)),
+    (ValueError, "one shape", lambda: A.block_norm(x, x[:3], w)),
+    (ValueError, "one shape", lambda: A.block_norm(torch.zeros(()), torch.zeros(()), w)),
+    (ValueError, "one shape", lambda: A.block_norm(torch.zeros(3, 0), torch.zeros(3, 0), w)),
+    (TypeError, "w_after", lambda: A.block_norm(x, x, w.bfloat16())),
+    (TypeError, "gate", lambda: A.block_norm(x, x, w, w, w.double())),
+    (ValueError, "w_before", lambda: A.block_norm(x, x, w, w[:4])),
+    (ValueError, "w_after", lambda: A.block_norm(x, x, w.view(1, 8))),
+    (ValueError, "gate", lambda: A.block_norm(x, x, w, w, torch.ones(2, 3, 8))),
+    (ValueError, "gate", lambda: A.block_norm(x, x, w, w, torch.ones(0, 8))),
+    (ValueError, "scale", lambda: A.block_norm(x, x, w, w, w, torch.ones(2, 2))),
+    (ValueError, "types", lambda: A.block_norm(x, x, w, w, torch.ones(2, 8), torch.ones(3), kinds)),
+    (ValueError, "types", lambda: A.block_norm(x, x, w, w, torch.ones(2, 8))),
+    (TypeError, "int32", lambda: A.block_norm(x, x, w, w, torch.ones(2, 8), None, kinds.long())),
+    (ValueError, "types", lambda: A.block_norm(x, x, w, w, torch.ones(2, 8), None, kinds[:3])),
+    (TypeError, "GPU", lambda: A.block_norm(x, x, w, w, torch.ones(2, 8), torch.ones(2), kinds)),
+    (TypeError, "CUDA", lambda: A.pack_rows(x)),
+    (TypeError, "int8", lambda: A.unpack_rows(x, x)),
+    (TypeError, "GPU", lambda: A.unpack_rows(x.char(), x.byte())),
+])
+def test_refused(kind, word, call):
+    with pytest.raises(kind, match=word):
+        call()
+
+
+def test_rows8_takes_what_it_is_made_for():
+    R = H.Rows8.__new__(H.Rows8)
+    R.rows, R.width, R._descs = 6, 8, {torch.float32: None, torch.bfloat16: None}
+    for bad in (x, x.half(), x[:3], x.t()):
+        with pytest.raises(TypeError, match="Rows8"):
+            R._desc(bad)

@@ -1,0 +1,308 @@
+"""The junction, rows in 8 bits and the feed-forward backward from them as a model uses them: a residual block around a relational layer with norms on both
+sides, gates by node type, and its training step.  Numbers against the same chain in 64 bits (the layer by the CPU oracle), to the tolerance of the layers' own
+tests; what holds rows in 8 bits against the C calls on the same rows, bit by bit."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import layers as O
+from paper_2412_04747_amd import synth
+from parity import check, TOL_F32
+
+pytestmark = pytest.mark.gpu
+
+
+def _problem(seed, N=700, R=5, E=6000, d=64, T=3):
+    import torch
+    rng, src, dst, rel, _ = synth.tiny(seed, N=N, R=R, E=E)
+    dst[:500] = 11
+    p = synth.rgat_params(rng, N, R, d, d)
+    types = torch.as_tensor(np.sort(rng.integers(0, T, N)).astype(np.int32))
+    return src, dst, rel, p, types
+
+
+def _modules(A, R, d, f, T, held):
+    import torch
+    torch.manual_seed(3)
+    conv, first, ffn = A.RgatConv(R, d), A.ResidualNorm(d), A.GatedFfn(d, f, held=held)
+    joins = [A.BlockNorm(d, T, gate=0.5, scale=0.9, held=held) for _ in range(2)]
+    for j in joins:
+        for q in j.parameters():
+            torch.nn.init.normal_(q, float(q.detach().mean()), 0.2)
+    return conv, first, ffn, joins
+
+
+def test_training_step_of_a_block():
+    """norm -> rgat -> junction -> feed-forward -> junction, its gradients, and their clipping."""
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    N, R, d, f, T = 700, 5, 64, 150, 3
+    src, dst, rel, p, types = _problem(411)
+    print(f"block training case N={N} R={R} d={d} f={f} T={T}", flush=True)
+    g = A.Graph(N, R, src, dst, rel)
+    conv, first, ffn, joins = _modules(A, R, d, f, T, False)
+    X = torch.tensor(p["X"], dtype=torch.float32, device="cuda", requires_grad=True)
+    dOut = torch.tensor(p["dOut"], dtype=torch.float32, device="cuda")
+    params = [q for m in (conv, first, ffn, *joins) for q in m.parameters()]
+    kinds = types.cuda()
+    y, s = joins[0](conv(g, first(X)), X, kinds)
+    out, s = joins[1](ffn(y), s, kinds)
+    (out * dOut + 0.3 * s * dOut).sum().backward()
+    grads = [q.grad.clone() for q in params]
+    norm = A.clip_grad_norm_(params, 0.7)
+    torch.cuda.synchronize()
+
+    class Layer(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, W, ws, wt):
+            ctx.save_for_backward(x, W, ws, wt)
+            return torch.from_numpy(O.rgat_fwd(N, src, dst, rel, *(t.detach().numpy() for t in (x, W, ws, wt))))
+
+        @staticmethod
+        def backward(ctx, dy):
+            b = O.rgat_bwd(N, src, dst, rel, *(t.detach().numpy() for t in ctx.saved_tensors), np.ascontiguousarray(dy.numpy()))
+            return tuple(torch.from_numpy(b[k]) for k in ("dX", "dW", "dw_s", "dw_t"))
+
+    q = [t.detach().cpu().double().requires_grad_() for t in (X, *params)]
+    x, W, ws, wt, w0, Wg, Wu, Wd, *rest = q
+    nrm = lambda t, w: t / torch.sqrt((t * t).mean(1, keepdim=True) + 1e-6) * w
+    k = types.long()
+
+    def join(a, s, w_after, w_before, gate, scale):
+        total = scale[k][:, None] * s + gate[k] * nrm(a, w_after)
+        return nrm(total, w_before), total
+
+    y, s = join(Layer.apply(nrm(x, w0), W, ws, wt), x, *rest[:4])
+    a = y @ Wg
+    want, s = join((a * torch.sigmoid(a) * (y @ Wu)) @ Wd, s, *rest[4:])
+    dO = dOut.cpu().double()
+    (want * dO + 0.3 * s * dO).sum().backward()
+    check(out, want.detach().numpy(), TOL_F32, "out")
+    check(X.grad, x.grad.numpy(), TOL_F32, "dX")
+    for i, (got, t) in enumerate(zip(grads, q[1:])):
+        check(got, t.grad.numpy(), TOL_F32, f"parameter {i}")
+    total = math.sqrt(sum(float((t.grad ** 2).sum()) for t in q[1:]))
+    assert abs(float(norm) - total) <= TOL_F32 * total and total > 0.7
+    g.close()
+
+
+def test_training_step_with_held_rows():
+    """The same block with rows held in 8 bits: outputs are the same bits, and every gradient is that of the C calls on the held rows."""
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    from paper_2412_04747_amd.harness import BlockNormLayer, FfnLayer, Rows8
+    N, d, f, T = 700, 64, 150, 3
+    _, _, _, p, types = _problem(412)
+    kinds = types.cuda()
+    torch.manual_seed(7)
+    a0, x0 = torch.randn(N, d, device="cuda"), torch.randn(N, d, device="cuda")
+    dO, dS = torch.randn(N, d, device="cuda"), torch.randn(N, d, device="cuda")
+    results = []
+    for held in (False, True):
+        _, _, ffn, joins = _modules(A, 5, d, f, T, held)
+        a, x = a0.clone().requires_grad_(), x0.clone().requires_grad_()
+        y, s = joins[0](a, x, kinds)
+        h = ffn(y)
+        out, s2 = joins[1](h, s, kinds)
+        torch.autograd.backward((out, s2), (dO, dS))
+        results.append((out.detach(), s2.detach(), a.grad, x.grad, [q.grad for m in (ffn, *joins) for q in m.parameters()], (y, s, h), ffn, joins))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    _, _, da, dx, grads, (y, s, h), ffn, joins = results[1]
+
+    def junction(m, a, s, dOut, dSum):
+        L = BlockNormLayer(N, d, types=T, held=True)
+        L.types, L.w_after, L.w_before, L.gate, L.scale = kinds, *(q.detach() for q in (m.weight_after, m.weight_before, m.gate, m.scale))
+        L.held_a.pack(a.detach())
+        L.held_s.pack(s.detach())
+        L.dOut, L.dSum = dOut, dSum
+        L.bwd()
+        return L
+
+    last = junction(joins[1], h, s, dO, dS)
+    F = FfnLayer(N, d, f)
+    F.held = Rows8(N, d)
+    F.held.pack(y.detach())
+    F.Wg, F.Wu, F.Wd, F.dOut = ffn.Wg.detach(), ffn.Wu.detach(), ffn.Wd.detach(), last.dA
+    F.bwd_held()
+    first = junction(joins[0], a0, x0, F.dX, last.dS)
+    torch.cuda.synchronize()
+    want = [F.dWg, F.dWu, F.dWd, *(t for L in (first, last) for t in (L.dWAfter, L.dWBefore, L.dGate, L.dScale))]
+    assert torch.equal(da, first.dA) and torch.equal(dx, first.dS)
+    for i, (got, w) in enumerate(zip(grads, want)):
+        assert torch.equal(got, w.view(got.shape)), i
+    # a rounding to 8 bits is half a step of at most 1/63 of a block's largest value: the gradients are near those of the rows themselves
+    for got, w in zip((da, dx, *grads), (*results[0][2:4], *results[0][4])):
+        assert torch.linalg.norm(got - w) <= 0.05 * torch.linalg.norm(w)
+
+
+@pytest.mark.parametrize("dtype,ratio", [("float32", 0.27), ("bfloat16", 0.53)])
+def test_bytes_kept_for_the_backward(dtype, ratio):
+    """What autograd keeps of rows of 128 columns: 33 bytes for 32 values and a type, against 128 or 64."""
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    t = getattr(torch, dtype)
+    N, d, f = 5000, 128, 64
+    kept = []
+    for held in (False, True):
+        torch.manual_seed(1)
+        join, ffn = A.BlockNorm(d, 2, out_dtype=t, held=held), A.GatedFfn(d, f, dtype=t, held=held)
+        a, s = (torch.randn(N, d, device="cuda").to(t).requires_grad_() for _ in range(2))
+        kinds = torch.zeros(N, dtype=torch.int32, device="cuda")
+        total = [0]
+
+        def pack(v):
+            total[0] += v.numel() * v.element_size() if v.dim() == 2 and v.shape[0] == N else 0
+            return v
+
+        with torch.autograd.graph.saved_tensors_hooks(pack, lambda v: v):
+            y, s2 = join(a, s, kinds)
+            out = ffn(y)
+        kept.append(total[0])
+        (out.float().sum() + s2.float().sum()).backward()
+        assert torch.isfinite(a.grad).all() and torch.isfinite(s.grad).all()
+    assert kept[1] <= ratio * kept[0], kept
+
+
+def test_skip_connection_by_node_type():
+    """HGT's learned skip: sigmoid(p[t]) a + (1 - sigmoid(p[t])) x, without norms: values and gradients against 64 bits.  Each value has two products, a sum and
+    the sigmoid's roundings: 8 units; a gradient of p is a sum over the rows of a type: 100 more."""
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    torch.manual_seed(2)
+    N, d, T = 900, 32, 4
+    U = 2.0 ** -24
+    a, x = (torch.randn(N, d, device="cuda", requires_grad=True) for _ in range(2))
+    p = torch.randn(T, device="cuda", requires_grad=True)
+    kinds = torch.randint(0, T, (N,), device="cuda", dtype=torch.int32)
+    g = torch.sigmoid(p)
+    out = A.block_norm(a, x, gate=g[:, None].expand(-1, d), scale=1 - g, types=kinds)
+    dO = torch.randn(N, d, device="cuda")
+    da, dx, dp = torch.autograd.grad(out, (a, x, p), dO)
+    q = [t.detach().cpu().double().requires_grad_() for t in (a, x, p)]
+    k = kinds.cpu().long()
+    s = torch.sigmoid(q[2])[k][:, None]
+    want = s * q[0] + (1 - s) * q[1]
+    wa, wx, wp = torch.autograd.grad(want, q, dO.cpu().double())
+    size = (s * q[0]).abs() + ((1 - s) * q[1]).abs() + q[1].abs()
+    assert ((out.cpu().double() - want).abs() <= 8 * U * size).all()
+    assert ((da.cpu().double() - wa).abs() <= 8 * U * wa.abs()).all() and ((dx.cpu().double() - wx).abs() <= 8 * U * (wx.abs() + dO.cpu().double().abs())).all()
+    terms = torch.zeros(T, dtype=torch.float64).index_add_(0, k, ((q[0].abs() + q[1].abs()) * dO.cpu().double().abs()).sum(1).detach())
+    assert ((dp.cpu().double() - wp).abs() <= 108 * U * terms).all()
+
+
+def test_shapes_strides_and_partial_gradients():
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    torch.manual_seed(6)
+    d, T = 32, 2
+    base = torch.randn(6, 7, d, device="cuda")
+    w1, w2, gate, scale = (torch.rand(*s, device="cuda") + 0.5 for s in ((d,), (d,), (T, d), (T,)))
+    views = {"leading dimensions": base, "transposed": base.transpose(0, 1), "every second": base[::2], "one row": base[0, 0],
+             "an offset of an element": torch.randn(5 * d + 1, device="cuda")[1:].view(5, d), "no rows": base[:0]}
+    for name, v in views.items():
+        flat = v.reshape(-1, d).contiguous().clone()
+        kinds = torch.randint(-1, T, v.shape[:-1], device="cuda", dtype=torch.int32)
+        want = A.block_norm(flat, flat, w1, w2, gate, scale, kinds.reshape(-1))
+        got = A.block_norm(v, v, w1, w2, gate, scale, kinds)
+        for g, w in zip(got, want):
+            assert torch.equal(g, w.view(v.shape)), name
+        codes, scales = A.pack_rows(v)
+        assert codes.shape == v.shape and scales.shape == (*v.shape[:-1], 1)
+        for t in (torch.float32, torch.bfloat16):
+            back = A.unpack_rows(codes, scales, t)
+            assert back.dtype == t and (back.float() - v).abs().max().nan_to_num() <= 4.0 / 126 if v.numel() else back.shape == v.shape
+        for held in (False, True):
+            a, s = v.detach().clone().requires_grad_(), v.detach().clone().requires_grad_()
+            o, t = A.block_norm(a, s, w1, w2, gate, scale, kinds, held=held)
+            (o.sum() + 2 * t.sum()).backward()
+            b, u = flat.clone().requires_grad_(), flat.clone().requires_grad_()
+            o, t = A.block_norm(b, u, w1, w2, gate, scale, kinds.reshape(-1), held=held)
+            torch.autograd.backward((o, t), (torch.ones_like(o), torch.full_like(t, 2.0)))
+            assert torch.equal(a.grad, b.grad.view(v.shape)) and torch.equal(s.grad, u.grad.view(v.shape)), name
+    # a gate of one row, a scale without dimensions, an expanded gate
+    flat = base.reshape(-1, d)
+    one = A.block_norm(flat, flat, w1, w2, gate[0], scale[0])
+    for g, s in ((gate[:1], scale[:1]), (gate[0].view(1, d).expand(1, d), scale[0])):
+        for x, y in zip(A.block_norm(flat, flat, w1, w2, g, s), one):
+            assert torch.equal(x, y)
+    # what needs no gradient gets none, and the others are the same
+    kinds = torch.randint(0, T, flat.shape[:1], device="cuda", dtype=torch.int32)
+    tensors = [t.clone() for t in (flat, flat + 1, w1, w2, gate, scale)]
+    full = [t.clone().requires_grad_() for t in tensors]
+    c, e = torch.randn_like(flat), torch.randn_like(flat)
+    o, t = A.block_norm(*full, kinds)
+    want = torch.autograd.grad((o * c).sum() + (t * e).sum(), full)
+    for i in range(6):
+        some = [t.clone().requires_grad_(k == i) for k, t in enumerate(tensors)]
+        o, t = A.block_norm(*some, kinds)
+        assert torch.equal(torch.autograd.grad((o * c).sum() + (t * e).sum(), some[i])[0], want[i]), i
+    # one of the results alone
+    o, t = A.block_norm(*full, kinds)
+    only_sum = torch.autograd.grad(t, full[:3], e, allow_unused=True)
+    o, t = A.block_norm(*full, kinds)
+    only_out = torch.autograd.grad(o, full[:3], c)
+    o, t = A.block_norm(*full, kinds)
+    both = torch.autograd.grad((o * c).sum() + (t * e).sum(), full[:3])
+    for x, y, z in zip(only_sum, only_out, both):
+        assert (x + y - z).abs().max() <= 1e-5 * (x.abs() + y.abs()).max()
+    # inputs that are not kept may be changed before the backward
+    a, s = (t.clone().requires_grad_() for t in tensors[:2])
+    h, r = a * 1, s * 1
+    o, t = A.block_norm(h, r, *tensors[2:], kinds, held=True)
+    with torch.no_grad():
+        h.zero_()
+        r.zero_()
+    (o.sum() + t.sum()).backward()
+    assert torch.isfinite(a.grad).all() and a.grad.any()
+
+
+def test_no_gradient_keeps_nothing():
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    x, w = torch.randn(50, 64, device="cuda"), torch.ones(64, device="cuda")
+    with torch.no_grad():
+        o, s = A.block_norm(x, x, w, w, held=True)
+        h = A.gated_ffn(x, *(torch.randn(n, m, device="cuda") for n, m in ((64, 20), (64, 20), (20, 64))), held=True)
+    assert o.grad_fn is None and h.grad_fn is None
+    o, s = A.block_norm(x, x, w, w, held=True)
+    assert o.grad_fn is None and not o.requires_grad
+
+
+def test_autograd_on_another_stream():
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    torch.manual_seed(9)
+    join, ffn = A.BlockNorm(64, 2, held=True), A.GatedFfn(64, 100, held=True)
+    x = torch.randn(500, 64, device="cuda")
+    kinds = torch.randint(0, 2, (500,), device="cuda", dtype=torch.int32)
+
+    def grads():
+        for q in (*join.parameters(), *ffn.parameters()):
+            q.grad = None
+        y, s = join(x, x, kinds)
+        (ffn(y) + s).square().sum().backward()
+        return [q.grad.clone() for q in (*join.parameters(), *ffn.parameters())]
+
+    want = grads()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = grads()
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_widths_that_the_library_refuses():
+    import torch
+    from paper_2412_04747_amd import autograd as A
+    from paper_2412_04747_amd.binding import RgnnError
+    x = torch.randn(2, 8193, device="cuda")
+    with pytest.raises(RgnnError, match="width"):
+        A.block_norm(x, x)
+    with pytest.raises(RgnnError, match="width"):
+        A.pack_rows(x)
+    with pytest.raises(RgnnError, match="types"):
+        A.block_norm(x[:, :64], x[:, :64], gate=torch.ones(54, 64, device="cuda"), types=torch.zeros(2, dtype=torch.int32, device="cuda"))
