@@ -38,7 +38,7 @@ struct BlockBwdArgs {
     const void* dy; const void* ds;
     void* da; void* dstream;
     int sums;                // whether a parameter's gradient is wanted
-    float* part;             // [gridDim.x][T + 1][columns, dscale]: G and dscale of each type, then dw2 (a single workgroup writes the gradients itself)
+    float* part;             // by groups of columns, [gridDim.x][T + 1] each: G and dscale of each type, then dw2 (a single workgroup writes the gradients itself)
     rgnn_block_norm_grads_t grads;
 };
 

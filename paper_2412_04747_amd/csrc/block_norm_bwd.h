@@ -27,6 +27,9 @@ constexpr int kTail = kBlock / 64;       // places behind a type's columns in th
 __host__ __device__ inline int columns4(int width) { return (width + 3) / 4 * 4; }
 __host__ __device__ inline int place_len(int width) { return columns4(width) + kTail; }
 __host__ __device__ inline int part_len(int width) { return columns4(width) + 4; }
+// Partial rows lie by groups of columns: [group][workgroup][T + 1][kReduceCols].
+constexpr int kReduceCols = 8;
+__host__ __device__ inline int part_groups(int width) { return (part_len(width) + kReduceCols - 1) / kReduceCols; }
 
 // i / n for i below 2^16 and a positive n
 __device__ __forceinline__ int quotient(int i, int n) { return (int)(((float)i + 0.5f) * (1.f / (float)n)); }
@@ -322,7 +325,8 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
         }
         if (c == L4 * 4 - 4) v = make_float4(v.x + v.y + v.z + v.w, 0.f, 0.f, 0.f);
         // (what another lane reads is in no lane's way: a place's vectors are read here by this lane alone)
-        *reinterpret_cast<float4*>(gridDim.x > 1 ? a.part + ((int64_t)blockIdx.x * (T + 1) + t) * part_len(a.width) + c : places + t * len + c) = v;
+        if (gridDim.x > 1) *reinterpret_cast<float4*>(a.part + (((int64_t)(c / kReduceCols) * gridDim.x + blockIdx.x) * (T + 1) + t) * kReduceCols + c % kReduceCols) = v;
+        else *reinterpret_cast<float4*>(places + t * len + c) = v;
     }
     if (gridDim.x > 1) return;
     __syncthreads();
