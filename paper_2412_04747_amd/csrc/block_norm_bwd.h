@@ -103,7 +103,7 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
     load_type(0);
     // adds a lane's sums to place t of its wavefront (workgroup); the lanes with `who`, those of a row together
     auto give = [&](bool who, int t, float (&v)[NV][V], float& tail) {
-        const float sum = lanes_sum(tail, min(sh.G, 64));
+        float sum = lanes_sum(tail, min(sh.G, 64));
         float* const at = mine + t * len;
         auto add = [&]() {
 #pragma unroll
@@ -125,6 +125,18 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
             return;
         }
         const unsigned long long which = __ballot(who);
+        if (which == ~0ull && __all(t == __builtin_amdgcn_readfirstlane(t))) {       // all of one type: their sum in one turn
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[j][e] = groups_sum(v[j][e], sh.G);
+            sum = groups_sum(sum, sh.G);
+            if ((threadIdx.x & 63) < (unsigned)sh.G) add();
+#pragma unroll
+            for (int j = 0; j < NV; ++j) zero_cols<V>(v[j]);
+            tail = 0.f;
+            return;
+        }
         for (int k = 0; k < 64; k += sh.G) {
             if (!((which >> k) & 1)) continue;
             if ((threadIdx.x & 63 & ~(sh.G - 1)) == (unsigned)k) add();
@@ -308,7 +320,12 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
         }
     }
     if (!a.sums) return;
-    give(type >= 0, max(type, 0), G, dscale);
+    // (lanes that never had a row hold zeros and go with the others)
+    const unsigned long long with_rows = __ballot(type >= 0);
+    if (with_rows) {
+        const int any = __shfl(type, __ffsll((unsigned long long)with_rows) - 1);
+        give(true, type >= 0 ? type : any, G, dscale);
+    }
     float unused = 0.f;
     give(true, T, dw2, unused);
     __syncthreads();

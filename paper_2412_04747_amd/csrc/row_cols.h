@@ -87,6 +87,17 @@ __device__ __forceinline__ float lanes_sum(float v, int G) {
     return v;
 }
 
+// Sum over a wavefront's lanes of the same number modulo G.
+__device__ __forceinline__ float groups_sum(float v, int G) {
+    if (G <= 1) v += dpp_move<kDppQuadSwap1>(v);
+    if (G <= 2) v += dpp_move<kDppQuadSwap2>(v);
+    if (G <= 4) v += dpp_move<kDppRowRotate + 4>(v);
+    if (G <= 8) v += dpp_move<kDppRowRotate + 8>(v);
+    if (G <= 16) v = half_rows_sum(v);
+    if (G <= 32) v = halves_sum(v);
+    return v;
+}
+
 // How a workgroup's lanes share rows: G lanes per row (kBlock: the whole workgroup).
 struct Shape {
     int G, rows_per_block, lane, group;
