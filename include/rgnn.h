@@ -383,7 +383,8 @@ rgnn_status_t rgnn_norm_bwd(const rgnn_norm_desc_t* desc, const void* sum, const
  * value is a whole number from -127 to 127 times it, the nearest (ties to even) to the value it stands for:
  *   x ~ code * 2^(scale - 133),   off by at most half a step;   codes int8 [rows, width], scales uint8 [rows, ceil(width / 32)]
  * The step is the least power of two, 2^-126 or more, with which the largest of the block rounds to at most 127; within half a step of 2^128, where
- * there is no larger scale, it is cut to 127.  An infinity or NaN makes its block NaN (scale 255).  Unpacked values are exact in either type. */
+ * there is no larger scale, it is cut to 127.  An infinity or NaN makes its block NaN (scale 255).  Unpacked values are exact in either type; scales below 7, which
+ * packing does not give, stand for zeros. */
 typedef struct {
     int8_t* codes;               /* 16-byte aligned */
     uint8_t* scales;

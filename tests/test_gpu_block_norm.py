@@ -33,7 +33,9 @@ CASES = [(1, 1, 1, "sorted", 0), (1, 64, 1, "sorted", 0), (3, 2, 2, "mixed", 0),
          (1000, 64, 4, "sorted", 0), (999, 64, 4, "mixed", 60), (129, 100, 2, "sorted", 0), (64, 128, 29, "mixed", 0), (700, 128, 29, "sorted", 9), (41, 255, 1, "sorted", 0),
          (30, 349, 7, "mixed", 3), (300, 349, 7, "sorted", 20), (77, 512, 1, "sorted", 0), (9, 1000, 4, "mixed", 1), (6, 1021, 1, "sorted", 0), (40, 1020, 3, "mixed", 4),
          (12, 2036, 2, "mixed", 1), (5, 2052, 1, "sorted", 0), (3, 4099, 1, "sorted", 0), (4, 8192, 1, "sorted", 0), (2, 8191, 1, "sorted", 0), (20011, 64, 5, "sorted", 100),
-         (9001, 1, 300, "mixed", 50), (6007, 16, 9, "mixed", 0)]
+         (9001, 1, 300, "mixed", 50), (6007, 16, 9, "mixed", 0),
+         # several turns of every workgroup: short vectors, rows of whole workgroups
+         (9000, 349, 7, "mixed", 40), (1200, 2052, 1, "sorted", 0), (1100, 1030, 3, "mixed", 17), (700, 4099, 1, "sorted", 0), (30000, 30, 3, "sorted", 11), (30000, 3, 2, "mixed", 7)]
 
 
 def inputs(rows, width, types, order, pad, a, total, out, seed):
@@ -360,20 +362,21 @@ def test_gradient_against_differences():
             assert abs((up - down) / (2 * h) - got) <= tol, (name, (up - down) / (2 * h), got, tol)
 
 
-def test_offsets_past_32_bits():
-    """2.2e9 elements in bf16: the last rows and the first."""
+@pytest.mark.parametrize("rows,width,dtype", [(17200000, 128, "bf16"), (900001, 64, "f32"), (600001, 100, "f32")])
+def test_many_rows(rows, width, dtype):
+    """2.2e9 elements in bf16, offsets past 32 bits; and results larger than the caches: the last rows and the first, with zeros between."""
     import torch
     from paper_2412_04747_amd.harness import BlockNormLayer
-    rows, width, k = 17200000, 128, 400
-    print(f"block_norm case rows={rows} width={width} bf16, large", flush=True)
-    d = inputs(2 * k, width, 1, "sorted", 0, "bf16", "bf16", "bf16", 18)
-    small = layer(d, 1, "bf16", "bf16", "bf16", held=True)
+    k = 400
+    print(f"block_norm case rows={rows} width={width} {dtype}, large", flush=True)
+    d = inputs(2 * k, width, 1, "sorted", 0, dtype, dtype, dtype, 18)
+    small = layer(d, 1, dtype, dtype, dtype, held=True)
     small.fwd()
     small.bwd()
-    L = BlockNormLayer(rows, width, "bf16", "bf16", "bf16", 1, EPS, held=True)
+    L = BlockNormLayer(rows, width, dtype, dtype, dtype, 1, EPS, held=True)
     L.w_after, L.w_before, L.gate, L.scale = small.w_after, small.w_before, small.gate, small.scale
     for name in ("a", "s", "dOut", "dSum"):
-        t = torch.zeros(rows, width, device="cuda", dtype=torch.bfloat16)
+        t = torch.zeros(rows, width, device="cuda", dtype=_t(dtype))
         t[:k], t[-k:] = getattr(small, name)[:k], getattr(small, name)[k:]
         setattr(L, name, t)
     L.fwd()
@@ -393,6 +396,32 @@ def _unpacked(held):
     t = torch.empty(held.rows, held.width, device="cuda")
     held.unpack(t)
     return t.cpu()
+
+
+@pytest.mark.parametrize("rows,width,types,order", [(5000, 64, 3, "mixed"), (300, 349, 7, "sorted"), (400, 2100, 1, "sorted"), (3, 64, 2, "mixed"), (4000, 1, 315, "mixed")])
+def test_nothing_is_written_past_the_buffers(rows, width, types, order):
+    """Workspace, gradients, results, codes and scales of exactly the sizes asked for, inside larger buffers whose other bytes stay."""
+    import torch
+    from paper_2412_04747_amd import binding as B
+    d = inputs(rows, width, types, order, 0, "f32", "f32", "f32", 19)
+    L = layer(d, types, "f32", "f32", "f32", held=True)
+    n = rows * width
+    sizes = dict(ws=B.rgnn_block_norm_workspace_bytes(L.desc), sum=4 * n, out=4 * n, dA=4 * n, dS=4 * n, dWAfter=4 * width, dWBefore=4 * width, dGate=4 * types * width,
+                 dScale=4 * types, ac=n, asc=rows * -(-width // 32), sc=n, ssc=rows * -(-width // 32))
+    bufs = {k: torch.full((v + 1024,), 0x5A, dtype=torch.uint8, device="cuda") for k, v in sizes.items()}
+    at = {k: b.data_ptr() for k, b in bufs.items()}
+    a8, s8 = B.rows8(at["ac"], at["asc"]), B.rows8(at["sc"], at["ssc"])
+    B.rgnn_block_norm_fwd(L.desc, L._params(), L.a, L.s, at["sum"], at["out"], a8, s8)
+    B.rgnn_block_norm_bwd(L.desc, L._params(), None, None, a8, s8, L.dOut, L.dSum, at["dA"], at["dS"],
+                          B.block_norm_grads(at["dWAfter"], at["dGate"], at["dScale"], at["dWBefore"]), at["ws"])
+    torch.cuda.synchronize()
+    for k, v in sizes.items():
+        assert (bufs[k][v:] == 0x5A).all(), k
+    L.fwd()
+    L.bwd()
+    torch.cuda.synchronize()
+    for k in ("sum", "out", *ALL):
+        assert torch.equal(bufs[k][:sizes[k]].view(torch.float32), getattr(L, k).flatten()), k
 
 
 def test_no_rows():

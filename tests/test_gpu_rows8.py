@@ -132,6 +132,29 @@ def test_captured_and_replayed_on_another_stream():
         assert np.array_equal(back.cpu().double().numpy(), reference(x.cpu().double().numpy())[2])
 
 
+def test_scales_at_any_address_and_bytes_that_nothing_writes():
+    """Scales may begin at any byte; below 7 they stand for zeros, and 255 for NaN whatever the codes are; a code of -128 is taken as it is."""
+    import torch
+    from paper_2412_04747_amd import binding as B
+    rows, width = 50, 70
+    x = _rows(rows, width, 4).cuda()
+    codes, raw = torch.zeros(rows, width, dtype=torch.int8, device="cuda"), torch.full((rows * 3 + 9,), 77, dtype=torch.uint8, device="cuda")
+    d = B.make_rows8_desc(rows, width)
+    B.rgnn_rows8_pack(d, x, B.rows8(codes, raw.data_ptr() + 3))
+    scales = raw[3:3 + rows * 3].view(rows, 3)
+    want = reference(x.cpu().double().numpy())
+    assert np.array_equal(codes.cpu().numpy(), want[0]) and np.array_equal(scales.cpu().numpy(), want[1])
+    assert (raw[:3] == 77).all() and (raw[-6:] == 77).all()
+    scales[0], scales[1], scales[2] = 0, 6, 255
+    codes[3, 5] = -128
+    back = torch.empty(rows, width, device="cuda")
+    B.rgnn_rows8_unpack(d, B.rows8(codes, raw.data_ptr() + 3), back)
+    torch.cuda.synchronize()
+    assert not back[:2].any() and torch.isnan(back[2]).all()
+    assert float(back[3, 5]) == -128 * 2.0 ** (int(scales[3, 0]) - 133)
+    assert np.array_equal(back[4:].cpu().double().numpy(), want[2][4:])
+
+
 def test_no_rows():
     from paper_2412_04747_amd.harness import Rows8
     import torch
