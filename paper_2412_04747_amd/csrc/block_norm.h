@@ -156,14 +156,15 @@ struct RowLanes {
         align<T>(j, w);
         raw_values<T, V>(w, v);
     }
-    // vector j of a row of fp32 that all rows share
+    // Vector j of a row of fp32 that all rows share.  A lane that has no column there reads the row's last vector.
     __device__ __forceinline__ void shared(const float* p, int j, float (&v)[V]) const {
         if constexpr (even) {
-            load_cols<V>(p + col(j), v);
+            load_cols<V>(p + min(col(j), width - V), v);
         } else if constexpr (S::LIE == kUneven) {
             RawCols<float, V> w;
             __builtin_memcpy(w, p + from(j), sizeof(w));
-            values<float>(j, w, v);
+            move_down<sizeof(float)>(w, min(col(j) - from(j), V - 1) * (int)sizeof(float));
+            raw_values<float, V>(w, v);
         } else {
             load_v<false>(p, col(j), width, v);
         }

@@ -80,23 +80,27 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
     float w2[NV][V], gw[NV][V], dw2[NV][V], G[NV][V], dscale = 0.f, scale = 1.f;
     auto load_type = [&](int t) {
         scale = a.p.scale ? a.p.scale[t] : 1.f;
+        float w[NV][V];
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (!sh.in(j)) continue;
-            float w[V];
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int e = 0; e < V; ++e) gw[j][e] = w[e] = 1.f;
-            if (a.p.gate) sh.shared(a.p.gate + (unsigned)(t * a.width), j, gw[j]);
-            if (a.p.w1) sh.shared(a.p.w1, j, w);
+            for (int e = 0; e < V; ++e) gw[j][e] = w[j][e] = 1.f;
+        // (lanes past the row's end load its last vector: all loads are on their way together)
+        if (a.p.gate)
 #pragma unroll
-            for (int e = 0; e < V; ++e) gw[j][e] *= w[e];
-        }
+            for (int j = 0; j < NV; ++j) sh.shared(a.p.gate + (unsigned)(t * a.width), j, gw[j]);
+        if (a.p.w1)
+#pragma unroll
+            for (int j = 0; j < NV; ++j) sh.shared(a.p.w1, j, w[j]);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < V; ++e) gw[j][e] = sh.in(j) ? gw[j][e] * w[j][e] : 0.f;
     };
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         zero_cols<V>(dw2[j]);
         zero_cols<V>(G[j]);
-        zero_cols<V>(gw[j]);
         zero_cols<V>(w2[j]);
         if (a.p.w2 && sh.in(j)) sh.shared(a.p.w2, j, w2[j]);
     }

@@ -229,6 +229,7 @@ class Rows8:
         self.codes = torch.empty(rows, width, device="cuda", dtype=torch.int8)
         self.scales = torch.empty(rows, -(-width // 32), device="cuda", dtype=torch.uint8)
         self._descs = {t: B.make_rows8_desc(rows, width, code) for t, code in _ROW_TYPES.items()}
+        self._table = B.rows8(None, None)         # (filled in at each call)
 
     def _desc(self, x):
         if x.dtype not in self._descs or not x.is_cuda or not x.is_contiguous() or x.numel() != self.rows * self.width:
@@ -236,7 +237,8 @@ class Rows8:
         return self._descs[x.dtype]
 
     def tensors(self):
-        return B.rows8(self.codes, self.scales)
+        self._table.codes, self._table.scales = self.codes.data_ptr(), self.scales.data_ptr()
+        return self._table
 
     def pack(self, x):
         B.rgnn_rows8_pack(self._desc(x), x, self.tensors(), _stream())
@@ -271,7 +273,8 @@ class BlockNormLayer:
         return (None, None) if self.held_a is None else (self.held_a.tensors(), self.held_s.tensors())
 
     def fwd(self):
-        B.rgnn_block_norm_fwd(self.desc, self._params(), self.a, self.s, self.sum, None if self.w_before is None else self.out, *self._held(), _stream())
+        a8, s8 = self._held()
+        B.rgnn_block_norm_fwd(self.desc, self._params(), self.a, self.s, self.sum, None if self.w_before is None else self.out, a8, s8, _stream())
 
     def bwd(self):
         a8, s8 = self._held()
