@@ -76,7 +76,8 @@ __device__ __forceinline__ void rows_block(const RowsArgs& r, int64_t block, uns
     // Operands are read from the LDS a step before they are multiplied.  The compiler would move the reads to their use and wait there; the
     // backward, whose registers are full, is left to it (2M rows, d 128, f 512, bf16, forward: 1061 us without the fences, 1050 with;
     // 200017 rows, f 341, backward: 300 and 306).
-    auto fence = [] { if constexpr (!BWD) __builtin_amdgcn_sched_barrier(0); };
+    // Rows held in 8 bits leave registers at width 128 in fp32, where the fences then pay: 300000 rows, f 341, dX alone: 715 us without, 668 with; 1M rows, d 64, f 170: 546 and 567.
+    auto fence = [] { if constexpr (!BWD || (HELD && D == 128 && PL == 3)) __builtin_amdgcn_sched_barrier(0); };
     struct FirstOps { bf16x8 f[BWD ? 3 : 2][PL]; };
     struct SecondOps { bf16x8 f[BWD ? 2 : 1][PL]; };
     auto read_first = [&](const unsigned char* w, int s) {
