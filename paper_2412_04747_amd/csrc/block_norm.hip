@@ -69,13 +69,15 @@ __global__ __launch_bounds__(block_threads(S::GC)) void block_fwd_kernel(BlockFw
     auto fetch = [&](int64_t row0, int t) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            if (t >= 0 && sh.in(j)) {
+                sh.template fetch<TA>(a.a, row0, j, xr[j]);
+                sh.template fetch<TS>(a.s, row0, j, sr[j]);
+            } else {
 #pragma unroll
-            for (int k = 0; k < (int)(sizeof(xr[j]) / 4); ++k) xr[j][k] = 0;
+                for (int k = 0; k < (int)(sizeof(xr[j]) / 4); ++k) xr[j][k] = 0;
 #pragma unroll
-            for (int k = 0; k < (int)(sizeof(sr[j]) / 4); ++k) sr[j][k] = 0;
-            if (t < 0 || !sh.in(j)) continue;
-            sh.template fetch<TA>(a.a, row0, j, xr[j]);
-            sh.template fetch<TS>(a.s, row0, j, sr[j]);
+                for (int k = 0; k < (int)(sizeof(sr[j]) / 4); ++k) sr[j][k] = 0;
+            }
         }
     };
     const int64_t step = (int64_t)gridDim.x * sh.rows();

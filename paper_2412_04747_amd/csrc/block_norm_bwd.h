@@ -65,7 +65,7 @@ template <typename TA, typename TS, typename TO, typename S, bool HELD>
 __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)) void block_bwd_kernel(BlockBwdArgs a) {
     extern __shared__ float lds[];           // row_sums' halves, then the places of the types
     constexpr int V = S::V, NV = S::NV, kThreads = block_threads(S::GC);
-    constexpr bool WIDE = S::GC == kBlock, AHEAD = V * NV <= 8, EVEN = S::LIE == kEven;
+    constexpr bool WIDE = S::GC == kBlock, AHEAD = V * NV <= 8, EVEN = S::LIE == kEven, STEPS = HELD && EVEN;
     constexpr int kWaves = kThreads / 64, slots = WIDE ? 1 : kWaves;
     const RowLanes<S> sh(a.G, a.width);
     const float inv = 1.f / (float)a.width;
@@ -193,14 +193,20 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
     // (the trip count is the same for all threads of a workgroup whose rows are its own: the barrier in row_sums)
     for (; row0 < a.rows; row0 += step) {
         if constexpr (!AHEAD) fetch(row0, t);
-        float x[NV][V], s[NV][V], dy[NV][V], dt[NV][V];
+        // Rows in 8 bits: x and s are their codes, a lane's all with one step (xs, ss), which its scalars take up (not of short vectors: their registers are full).
+        float x[NV][V], s[NV][V], dy[NV][V], dt[NV][V], xs[NV], ss[NV];
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
+            xs[j] = ss[j] = 1.f;
             if constexpr (HELD) {
                 sh.template align<int8_t>(j, xc[j]);
                 sh.template align<int8_t>(j, sc[j]);
-                from_codes<V>(xc[j], held_step(xb[j]), x[j]);
-                from_codes<V>(sc[j], held_step(sb[j]), s[j]);
+                if constexpr (STEPS) {
+                    xs[j] = held_step(xb[j]);
+                    ss[j] = held_step(sb[j]);
+                }
+                from_codes<V>(xc[j], STEPS ? 1.f : held_step(xb[j]), x[j]);
+                from_codes<V>(sc[j], STEPS ? 1.f : held_step(sb[j]), s[j]);
             } else {
                 sh.template values<TA>(j, xr[j], x[j]);
                 sh.template values<TS>(j, sr[j], s[j]);
@@ -229,32 +235,44 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
         if (a.p.w1) {
             float sq = 0.f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j) sq += dot_cols<V>(x[j], x[j]);
+            for (int j = 0; j < NV; ++j) sq += dot_cols<V>(x[j], x[j]) * xs[j] * xs[j];
             row_sum(sq, sh.G, lds, turn++);
             if (!(sq <= FLT_MAX)) {          // as in the forward; the scaled values take their place
                 k1 = kScaleDown;
                 sq = 0.f;
 #pragma unroll
-                for (int j = 0; j < NV; ++j)
+                for (int j = 0; j < NV; ++j) {
+                    if constexpr (STEPS) {
+                        xs[j] *= k1;
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        x[j][e] *= k1;
-                        sq += x[j][e] * x[j][e];
+                        for (int e = 0; e < V; ++e) x[j][e] *= k1;
                     }
+                    sq += dot_cols<V>(x[j], x[j]) * xs[j] * xs[j];
+                }
                 row_sum(sq, sh.G, lds, turn++);
             }
             q1 = rsqrtf(sq * inv + a.eps * k1 * k1);
         }
+        // x: from here on a q1
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const float by = STEPS ? q1 * xs[j] : q1;
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[j][e] *= by;
+        }
         if (a.dy) {
             float u[NV][V], sq = 0.f, gs = 0.f;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j) {
+                const float by = STEPS ? scale * ss[j] : scale;
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    u[j][e] = scale * s[j][e] + x[j][e] * q1 * gw[j][e];
+                    u[j][e] = by * s[j][e] + x[j][e] * gw[j][e];
                     sq += u[j][e] * u[j][e];
                     gs += dy[j][e] * w2[j][e] * u[j][e];
                 }
+            }
             row_sums(sq, gs, sh.G, lds, turn++);
             float k2 = 1.f;
             if (!(sq <= FLT_MAX)) {
@@ -282,45 +300,68 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
                     }
             }
         }
+        auto out = [&](auto* to, int j, const float (&v)[V]) {
+            if constexpr (EVEN)
+                if (a.streaming) return store_cols_nt<V>(to + sh.col(j), v);
+            put<EVEN>(to, sh.col(j), a.width, v, a.accumulate);
+        };
+        TA* const da_row = sh.template row<TA>(a.da, row0);
+        TS* const ds_row = sh.template row<TS>(a.dstream, row0);
+        // dS, and what the row adds to its type's sums
+        auto stream = [&]() {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (!sh.in(j)) continue;
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    v[e] = scale * dt[j][e];
+                    G[j][e] += dt[j][e] * x[j][e];
+                }
+                dscale += dot_cols<V>(dt[j], s[j]) * ss[j];
+                if (a.dstream) out(ds_row, j, v);
+            }
+        };
+        // (dS before the last sum, which leaves h in dT's place; short vectors' stores take ways of their own, and once is enough)
+        constexpr bool SOON = EVEN;
+        if (SOON && now >= 0) stream();
         float along = 0.f;
-        if (a.p.w1) {
-            float ha = 0.f;
+        if (SOON || a.p.w1) {
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int e = 0; e < V; ++e) ha += dt[j][e] * gw[j][e] * x[j][e];
-            row_sum(ha, sh.G, lds, turn++);
-            along = q1 * q1 * (ha * inv);
-        }
-        if (!live || (now < 0 && a.accumulate)) continue;
-        const float qk = q1 * k1;
-        TA* const da_row = sh.template row<TA>(a.da, row0);
-        TS* const ds_row = sh.template row<TS>(a.dstream, row0);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (!sh.in(j)) continue;
-            float da[V], dstream[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                da[e] = now >= 0 ? qk * (dt[j][e] * gw[j][e] - x[j][e] * along) : 0.f;
-                dstream[e] = scale * dt[j][e];
-            }
-            if (now >= 0) {
-#pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    G[j][e] += dt[j][e] * (x[j][e] * q1);
-                    dscale += dt[j][e] * s[j][e];
+                    const float h = dt[j][e] * gw[j][e];
+                    along += h * x[j][e];
+                    if constexpr (SOON) dt[j][e] = h;
                 }
-            } else {
-                zero_cols<V>(dstream);
+        }
+        if (a.p.w1) {
+            row_sum(along, sh.G, lds, turn++);
+            along *= inv;
+        } else {
+            along = 0.f;
+        }
+        if (now >= 0) {
+            const float qk = q1 * k1;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (!a.da || !sh.in(j)) continue;
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = qk * ((SOON ? dt[j][e] : dt[j][e] * gw[j][e]) - x[j][e] * along);
+                out(da_row, j, v);
             }
-            auto out = [&](auto* to, const float (&v)[V]) {
-                if constexpr (EVEN)
-                    if (a.streaming) return store_cols_nt<V>(to + sh.col(j), v);
-                put<EVEN>(to, sh.col(j), a.width, v, a.accumulate);
-            };
-            if (a.da) out(da_row, da);
-            if (a.dstream) out(ds_row, dstream);
+            if (!SOON) stream();
+        } else if (live && !a.accumulate) {
+            float none[V];
+            zero_cols<V>(none);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (!sh.in(j)) continue;
+                if (a.da) out(da_row, j, none);
+                if (a.dstream) out(ds_row, j, none);
+            }
         }
     }
     if (!a.sums) return;
