@@ -6,6 +6,9 @@
 // Sums over rows: a lane keeps its columns' G and dw2 in registers while its rows have one type.  Where the type changes it adds G to the place of
 // that type in the LDS, which is its wavefront's (lanes of one wavefront that share columns take turns), so that no order depends on timing.  Nodes are
 // mostly stored type by type: then that is rare.  A workgroup leaves one partial row per type; a second launch adds those in order.
+// Against 4.9 TB/s of a large copy: 1M rows of 64, fp32, four types, 280 us (5.5 TB/s; from 8 bits 209, 5.5; in mixed order 285); 2M rows of 128, bf16, 560 (4.6; from
+// 8 bits 465, 5.5); 30011 rows of 349, fp32, 67 (3.7), seven mixed types 78.  Before the next row's tensors were fetched while a row is worked on, and the
+// addresses had 32 bits of their own, the same kernel took 1000 us for 2M rows of 128 from 8 bits.
 #pragma once
 #include <float.h>
 
@@ -17,7 +20,8 @@ namespace rgnn {
 
 namespace {
 
-// Wavefronts that share a SIMD.  The registers of 4 columns per lane would allow five, of 8 three: with the next row's tensors on their way three are enough.
+// Wavefronts that share a SIMD.  With the next row's tensors on their way three are enough, and more only spread what is read at a time: the registers of 4 columns per
+// lane would allow four (1M rows of 64, fp32: 316 us with four, 303 with three; of 8 columns, from 8 bits: 520 with three, 545 with two).
 constexpr int per_simd(int cols, int GC) { return GC == kBlock || cols > 8 ? 2 : 3; }
 constexpr size_t kLdsBytes = 160 * 1024;      // of a compute unit
 constexpr int kSumsLds = 4 * (kBlock / 64);
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
             if (c == L4 * 4 - 4) add(at[1]);
         }
         if (c == L4 * 4 - 4) v = make_float4(v.x + v.y + v.z + v.w, 0.f, 0.f, 0.f);
-        // (what another lane reads is in no lane's way: a place's vectors are read here by this lane alone)
+        // (each place's vectors are read by one lane alone, which may write there)
         if (gridDim.x > 1) *reinterpret_cast<float4*>(a.part + (((int64_t)(c / kReduceCols) * gridDim.x + blockIdx.x) * (T + 1) + t) * kReduceCols + c % kReduceCols) = v;
         else *reinterpret_cast<float4*>(places + t * len + c) = v;
     }
