@@ -6,8 +6,8 @@
 // Sums over rows: a lane keeps its columns' G and dw2 in registers while its rows have one type.  Where the type changes it adds G to the place of
 // that type in the LDS, which is its wavefront's (lanes of one wavefront that share columns take turns), so that no order depends on timing.  Nodes are
 // mostly stored type by type: then that is rare.  A workgroup leaves one partial row per type; a second launch adds those in order.
-// Against 4.9 TB/s of a large copy: 1M rows of 64, fp32, four types, 280 us (5.5 TB/s; from 8 bits 209, 5.5; in mixed order 285); 2M rows of 128, bf16, 560 (4.6; from
-// 8 bits 465, 5.5); 30011 rows of 349, fp32, 67 (3.7), seven mixed types 78.  Before the next row's tensors were fetched while a row is worked on, and the
+// Against 4.9 TB/s of a large copy: 1M rows of 64, fp32, four types, 272 us (5.7 TB/s; from 8 bits 212, 5.5; in mixed order 282); 2M rows of 128, bf16, 562 (5.5; from
+// 8 bits 463, 5.6); 30011 rows of 349, fp32, 65 (3.8), seven mixed types 82.  Before the next row's tensors were fetched while a row is worked on, and the
 // addresses had 32 bits of their own, the same kernel took 1000 us for 2M rows of 128 from 8 bits.
 #pragma once
 #include <float.h>
@@ -21,7 +21,7 @@ namespace rgnn {
 namespace {
 
 // Wavefronts that share a SIMD.  With the next row's tensors on their way three are enough, and more only spread what is read at a time: the registers of 4 columns per
-// lane would allow four (1M rows of 64, fp32: 316 us with four, 303 with three; of 8 columns, from 8 bits: 520 with three, 545 with two).
+// lane would allow four (1M rows of 64, fp32: 314 us with four, 301 with three; of 8 columns, from 8 bits: 520 with three, 545 with two).
 constexpr int per_simd(int cols, int GC) { return GC == kBlock || cols > 8 ? 2 : 3; }
 constexpr size_t kLdsBytes = 160 * 1024;      // of a compute unit
 constexpr int kSumsLds = 4 * (kBlock / 64);
