@@ -48,13 +48,14 @@ __device__ __forceinline__ void raw_values(const RawCols<T, V>& w, float (&v)[V]
     for (int e = 0; e < V; ++e)
         v[e] = __uint_as_float(sizeof(T) == 4 ? w[e * sizeof(T) / 4] : e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
 }
-// Moves the elements of SIZE bytes in words down by `bytes`, fewer than there are, zeros after them.
+// Moves the elements of SIZE bytes in words down by `bytes`, fewer than there are, zeros after them.  (Lanes past a row's end come with zeros and any `bytes`: a shift
+// is defined for them too.)
 template <int SIZE, int N>
 __device__ __forceinline__ void move_down(unsigned (&w)[N], int bytes) {
     if constexpr (N == 1) {
-        w[0] >>= 8 * bytes;
+        w[0] >>= 8 * (bytes & 3);
     } else if constexpr (N == 2) {
-        const unsigned long long v = ((unsigned long long)w[1] << 32 | w[0]) >> (8 * bytes);
+        const unsigned long long v = ((unsigned long long)w[1] << 32 | w[0]) >> (8 * (bytes & 7));
         w[0] = (unsigned)v;
         w[1] = (unsigned)(v >> 32);
     } else {
