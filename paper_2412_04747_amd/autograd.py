@@ -201,6 +201,12 @@ class _ResidualNorm(torch.autograd.Function):
         return None, None, dX if need_x else None, (dX if same else dR) if need_r else None, dW
 
 
+def _held(wanted):
+    """Whether rows are to be held in 8 bits: only where a graph may be recorded.  (Within a Function's forward grad mode is off, and parameters ask for
+    gradients whether or not there is one.)"""
+    return bool(wanted) and torch.is_grad_enabled()
+
+
 def _pack(x):
     """(codes, scales) of contiguous rows in 8 bits."""
     width = x.shape[-1]
@@ -288,7 +294,7 @@ def block_norm(a, s, w_after=None, w_before=None, gate=None, scale=None, types=N
     the norm before the next.  sum has s's type, out has out_dtype (fp32 or bf16; default: a's).  A row whose type is not one of the parameters' stands for
     nothing (a batch's padding): it is not read, and its results and gradients are zeros.
     HGT's skip connection: gate = sigmoid(p)[:, None].expand(-1, width), scale = 1 - sigmoid(p).
-    held: a and s are kept for the backward in 8 bits."""
+    held: a and s are kept for the backward in 8 bits (without a backward, nothing is packed)."""
     if out_dtype is not None and out_dtype not in _CODES:
         raise TypeError(f"block_norm: out_dtype is fp32 or bf16, not {out_dtype}")
     for t in (a, s):
@@ -318,7 +324,7 @@ def block_norm(a, s, w_after=None, w_before=None, gate=None, scale=None, types=N
     for t in (a, s, w_after, w_before, gate, scale, types):
         if t is not None and (not t.is_cuda or t.device != a.device):
             raise TypeError("block_norm takes tensors on one GPU")
-    return _BlockNorm.apply(float(eps), out_dtype or a.dtype, bool(held), num_types, types, a, s, w_after, w_before, gate, scale)
+    return _BlockNorm.apply(float(eps), out_dtype or a.dtype, _held(held), num_types, types, a, s, w_after, w_before, gate, scale)
 
 
 class _GatedFfn(torch.autograd.Function):
@@ -366,10 +372,10 @@ def residual_norm(x, weight, residual=None, eps=1e-6, out_dtype=None):
 
 def gated_ffn(X, Wg, Wu, Wd, act="silu", held=False):
     """Gated feed-forward block (act(X Wg) * (X Wu)) Wd over the last dimension; Wg, Wu [d, hidden], Wd [hidden, d], all of X's type.
-    held: X is kept for the backward in 8 bits."""
+    held: X is kept for the backward in 8 bits (without a backward, nothing is packed)."""
     if act not in ("silu", "relu"):
         raise ValueError(f"gated_ffn: unknown activation {act!r}")
-    return _GatedFfn.apply(act, bool(held), X, Wg, Wu, Wd)
+    return _GatedFfn.apply(act, _held(held), X, Wg, Wu, Wd)
 
 
 def _apart(t):

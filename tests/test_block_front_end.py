@@ -43,3 +43,20 @@ def test_rows8_takes_what_it_is_made_for():
     for bad in (x, x.half(), x[:3], x.t()):
         with pytest.raises(TypeError, match="Rows8"):
             R._desc(bad)
+
+
+@pytest.mark.parametrize("grad_mode", ["no_grad", "inference_mode", "enabled"])
+def test_rows_are_held_only_for_a_backward(grad_mode, monkeypatch):
+    """Parameters ask for gradients in evaluation too: whether a graph is recorded decides."""
+    asked = {}
+    monkeypatch.setattr(A._BlockNorm, "apply", staticmethod(lambda *args: asked.update(block=args[2])))
+    monkeypatch.setattr(A._GatedFfn, "apply", staticmethod(lambda *args: asked.update(ffn=args[1])))
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    weights = [torch.nn.Parameter(torch.ones(*shape)) for shape in ((8,), (8, 4), (8, 4), (4, 8))]
+    with {"no_grad": torch.no_grad, "inference_mode": torch.inference_mode, "enabled": torch.enable_grad}[grad_mode]():
+        A.block_norm(x, x, weights[0], held=True)
+        A.gated_ffn(x, *weights[1:], held=True)
+        assert asked == dict(block=grad_mode == "enabled", ffn=grad_mode == "enabled")
+        A.block_norm(x, x, weights[0])
+        A.gated_ffn(x, *weights[1:])
+        assert asked == dict(block=False, ffn=False)
