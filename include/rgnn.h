@@ -403,7 +403,8 @@ rgnn_status_t rgnn_rows8_unpack(const rgnn_rows8_desc_t* desc, const rgnn_rows8_
  * row by row, t = types[row].  HGT's learned skip connection is gate[t] = sigmoid(p[t]), scale[t] = 1 - sigmoid(p[t]); a layer scale is one gate row.
  * a_dtype: a, dA.  sum_dtype: s, sum, dSum, dS.  out_dtype: out, dOut.  Types of tensors, sums and in-range rows as for rgnn_norm_*; parameters
  * and their gradients are fp32.
- *   types      1, or so many rows of gate and scale that types * (width + 12) <= 4096
+ *   types      1, or so many rows of gate and scale that types * (width + 12) <= 4096, or, up to 32 of them with width up to 1024, that
+ *              (types + 1) * (width + 12) <= 9600
  *   flags      0 or RGNN_FLAG_ACCUMULATE (backward: every gradient is added to) */
 typedef struct {
     int64_t rows;                /* below 2^31 */

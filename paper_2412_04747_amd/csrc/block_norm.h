@@ -62,6 +62,13 @@ inline JunctionPlan block_plan(const rgnn_block_norm_desc_t* d) {
     return p;
 }
 
+// Types whose sums a backward's workgroup can hold in the LDS at once: four places of each, or one where a row is a workgroup's (block_norm_bwd.h).  The first bound leaves two
+// workgroups of narrow rows to a compute unit; within the second, up to 154 KB, there may be one.  (Backward, fp32, with 1, 3 and 8 types in order: 50000 rows of 1024 in 214, 219 and
+// 244 us; with 3 and 8 mixed 225 and 249; 100000 rows of 512 with 4, 7 and 8 types 224, 217 and 232.)
+inline bool block_types_fit(int64_t types, int64_t width) {
+    return types == 1 || types * (width + 12) <= 4096 || (types <= 32 && width <= 1024 && (types + 1) * (width + 12) <= 9600);
+}
+
 // How vectors lie in a row: its width is a multiple of them; or the last one is short; or there is only that.
 enum Lie { kUneven, kEven, kNarrow };
 

@@ -190,8 +190,9 @@ rgnn_status_t check_desc(const rgnn_block_norm_desc_t* d) {
     if (d->width > kMaxWidth) RGNN_FAIL(RGNN_EUNSUPPORTED, "width %d not supported (up to %d)", d->width, kMaxWidth);
     for (int32_t t : {d->a_dtype, d->sum_dtype, d->out_dtype}) RGNN_TRY(check_dtype(t));
     if (d->types < 1) RGNN_FAIL(RGNN_EINVAL, "types %d is not positive", d->types);
-    if (d->types > 1 && (int64_t)d->types * (d->width + 12) > 4096)
-        RGNN_FAIL(RGNN_EUNSUPPORTED, "types %d of width %d not supported (types * (width + 12) up to 4096)", d->types, d->width);
+    if (!block_types_fit(d->types, d->width))
+        RGNN_FAIL(RGNN_EUNSUPPORTED, "types %d of width %d not supported (types * (width + 12) up to 4096; up to 32 types of up to 1024 columns: (types + 1) * (width + 12) up to 9600)",
+                  d->types, d->width);
     if (!(d->eps >= 0.f) || d->eps == INFINITY) RGNN_FAIL(RGNN_EINVAL, "eps is not a finite number >= 0");
     if (d->flags & ~RGNN_FLAG_ACCUMULATE) RGNN_FAIL(RGNN_EINVAL, "flags: only RGNN_FLAG_ACCUMULATE applies");
     return RGNN_OK;

@@ -400,7 +400,7 @@ __global__ __launch_bounds__(block_threads(S::GC), per_simd(S::V * S::NV, S::GC)
 }
 
 inline size_t lds_bytes(const rgnn_block_norm_desc_t* d, const JunctionPlan& p, bool sums) {
-    // (places of types * (width + 12) <= 4096, four of them at most: 82 KB)
+    // (four places of each type, (types + 1) * (width + 12) <= 9600 together: 154 KB at most; or one: 82)
     return sizeof(float) * (kSumsLds + (sums ? (size_t)(p.G == kBlock ? 1 : block_threads(p.G) / 64) * (d->types + 1) * place_len(d->width) : 0));
 }
 // As many as are resident at once, so that none comes in a second turn.  (What two turns of a workgroup finish is left to one: the sums then need no second launch.)

@@ -475,3 +475,31 @@ def test_captured_and_replayed_on_another_stream():
         for _, L in graphs:
             for n in ("sum", "out", *ALL):
                 assert torch.equal(getattr(L, n), getattr(eager, n)), n
+
+
+# types whose places take most of a compute unit's LDS: one and several workgroups, vectors of four and of eight, rows of odd widths, types without a row
+MANY_TYPES = [(700, 512, 8, "mixed", 20), (4000, 512, 8, "sorted", 30), (300, 1000, 5, "mixed", 3), (90, 1021, 7, "sorted", 2), (600, 1024, 8, "mixed", 11), (2500, 1024, 8, "sorted", 40),
+              (5, 1024, 8, "mixed", 1), (9000, 128, 32, "mixed", 50), (20000, 128, 30, "sorted", 100), (60, 277, 32, "mixed", 4), (1, 600, 8, "sorted", 0)]
+
+
+@pytest.mark.parametrize("dtypes", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f32", "bf16", "bf16")])
+@pytest.mark.parametrize("rows,width,types,order,pad", MANY_TYPES)
+def test_many_types_of_wide_rows(rows, width, types, order, pad, dtypes):
+    """Forward and backward, from the rows themselves and from 8 bits, and the same bits when the backward is called again."""
+    import torch
+    print(f"block_norm case rows={rows} width={width} types={types} {order} pad={pad}, {dtypes}", flush=True)
+    d = inputs(rows, width, types, order, pad, *dtypes, 5 * rows + width)
+    held = layer(d, types, *dtypes, held=True)
+    for L in (layer(d, types, *dtypes), held):
+        r, m = definition(d, types)
+        L.fwd()
+        within(L, d, r, m, ("sum", "out"))
+        if L is held:
+            r, m = definition(d, types, held={"a": _unpacked(L.held_a), "s": _unpacked(L.held_s)})
+        L.bwd()
+        within(L, d, r, m, ALL)
+        want = [getattr(L, n).clone() for n in ALL]
+        L.bwd()
+        torch.cuda.synchronize()
+        for n, w in zip(ALL, want):
+            assert torch.equal(getattr(L, n), w), n

@@ -167,3 +167,23 @@ def test_declared_argument_counts():
     for name, args in re.findall(r"\b(rgnn_\w+)\s*\(([^;]*?)\)\s*;", header, re.S):
         if name in B._ROW_OPS:
             assert len(args.split(",")) == len(B._ROW_OPS[name]), name
+
+
+def test_block_norm_of_every_drawn_workload():
+    """Up to 8 types of up to 1024 columns, as the workloads draw them, and what lies between."""
+    import random
+    from perf import more_operators as M
+    code = dict(f32=B.RGNN_F32, bf16=B.RGNN_BF16)
+    rng = random.Random(5)
+    wide = 0
+    for c in [*M.listed(), *(M.draw(rng) for _ in range(6000))]:
+        if c["op"] == "block":
+            wide += c["types"] > 1 and c["types"] * (c["width"] + 12) > 4096
+            d = desc(rows=c["rows"], width=c["width"], types=c["types"], a_dtype=code[c["a"]], sum_dtype=code[c["total"]], out_dtype=code[c["out"]])
+            assert B.rgnn_block_norm_workspace_bytes(d) > 0, c
+    assert wide > 5
+    for types, width in ((8, 1024), (8, 512), (5, 1000), (4, 1024), (2, 1024), (30, 128), (32, 278), (16, 552)):
+        for t in code.values():
+            assert B.rgnn_block_norm_workspace_bytes(desc(types=types, width=width, rows=100000, a_dtype=t, sum_dtype=t, out_dtype=t)) > 0
+    for types, width in ((9, 1024), (33, 200), (32, 279), (4, 1025)):
+        refused(EUNSUPPORTED, "types", B.rgnn_block_norm_workspace_bytes, desc(types=types, width=width))
