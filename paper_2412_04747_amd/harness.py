@@ -218,11 +218,36 @@ class NormLayer:
 
 
 _ROW_TYPES = {torch.float32: B.RGNN_F32, torch.bfloat16: B.RGNN_BF16}
+_STORED = {code: t for t, code in _ROW_TYPES.items()}
+
+
+class _Checked:
+    """A buffer that callers may put their own in the place of: its type, size, order and place are looked at when it is set.  want(owner): its type and number of
+    elements.  (Reads find the tensor itself in the owner.)"""
+
+    def __init__(self, want, optional=True):
+        self.want, self.optional = want, optional
+
+    def __set_name__(self, owner, name):
+        self.name = name
+
+    def __set__(self, owner, t):
+        if t is owner.__dict__.get(self.name, self):
+            return
+        if t is not None or not self.optional:
+            dtype, n = self.want(owner)
+            if t is None or t.dtype != dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+                raise TypeError(f"{type(owner).__name__}.{self.name}: {n} contiguous elements in {dtype} on the GPU are wanted"
+                                + ("" if t is None else f", not {tuple(t.shape)} in {t.dtype}"))
+        owner.__dict__[self.name] = t
 
 
 class Rows8:
     """Buffers for `rows` rows held in 8 bits: `codes` int8 [rows, width], `scales` uint8 [rows, blocks of 32 columns].  Both may be replaced by the
     caller's own."""
+
+    codes = _Checked(lambda r: (torch.int8, r.rows * r.width), optional=False)
+    scales = _Checked(lambda r: (torch.uint8, r.rows * -(-r.width // 32)), optional=False)
 
     def __init__(self, rows, width):
         self.rows, self.width = rows, width
@@ -251,6 +276,14 @@ class BlockNormLayer:
     """Device buffers for one junction call pair on `rows` rows: norm after a block, gate and residual scale by node type, norm before the next.  `a`, `s`
     (and `dOut`, `dSum`), the parameters and `types` (int32, with more than one) are set by the caller; types "f32" or "bf16".  held: the forward leaves
     a and s in 8 bits (`held_a`, `held_s`), and the backward reads them there."""
+
+    _rows = lambda code: _Checked(lambda L: (_STORED[getattr(L.desc, code)], L.desc.rows * L.desc.width))
+    a, s, dOut, dSum = _rows("a_dtype"), _rows("sum_dtype"), _rows("out_dtype"), _rows("sum_dtype")
+    types = _Checked(lambda L: (torch.int32, L.desc.rows))
+    w_after, w_before = (_Checked(lambda L: (torch.float32, L.desc.width)) for _ in range(2))
+    gate = _Checked(lambda L: (torch.float32, L.desc.types * L.desc.width))
+    scale = _Checked(lambda L: (torch.float32, L.desc.types))
+    del _rows
 
     def __init__(self, rows, width, a="f32", total="f32", out="f32", types=1, eps=1e-6, held=False, flags=0):
         (ca, ta), (cs, ts), (co, to) = _tdtype(a), _tdtype(total), _tdtype(out)
@@ -303,6 +336,8 @@ class FfnLayer:
         B.rgnn_ffn_bwd(self.desc, self.X, self.Wg, self.Wu, self.Wd, self.dOut, self.dX, self.dWg, self.dWu, self.dWd, self.ws, _stream())
 
     def bwd_held(self):
+        if (self.held.rows, self.held.width) != (self.desc.rows, self.desc.width):
+            raise ValueError(f"FfnLayer: held rows are [{self.held.rows}, {self.held.width}], not [{self.desc.rows}, {self.desc.width}]")
         B.rgnn_ffn_bwd_rows8(self.desc, self.held.tensors(), self.Wg, self.Wu, self.Wd, self.dOut, self.dX, self.dWg, self.dWu, self.dWd, self.ws, _stream())
 
     def grads(self):

@@ -60,3 +60,35 @@ def test_rows_are_held_only_for_a_backward(grad_mode, monkeypatch):
         A.block_norm(x, x, weights[0])
         A.gated_ffn(x, *weights[1:])
         assert asked == dict(block=False, ffn=False)
+
+
+def test_buffers_of_the_harness(monkeypatch):
+    """What a caller puts in a buffer's place has its type and size: a kernel writes or reads all of it."""
+    from paper_2412_04747_amd import binding as B
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    R = H.Rows8.__new__(H.Rows8)
+    R.rows, R.width = 6, 40
+    good = dict(codes=torch.zeros(6, 40, dtype=torch.int8), scales=torch.zeros(6, 2, dtype=torch.uint8))
+    L = H.BlockNormLayer.__new__(H.BlockNormLayer)
+    L.desc = B.make_block_norm_desc(6, 40, B.RGNN_F32, B.RGNN_BF16, B.RGNN_BF16, 3)
+    rows = torch.zeros(6, 40)
+    block = dict(a=rows, s=rows.bfloat16(), dOut=rows.bfloat16(), dSum=rows.bfloat16(), types=torch.zeros(6, dtype=torch.int32), w_after=torch.ones(40),
+                 w_before=torch.ones(40), gate=torch.ones(3, 40), scale=torch.ones(3))
+    for owner, tensors in ((R, good), (L, block)):
+        for name, t in tensors.items():
+            setattr(owner, name, t)
+            assert getattr(owner, name) is t
+            for bad in (t[:-1], torch.cat([t, t]), t.double(), t.repeat_interleave(2, -1)[..., ::2], t.long(), None if owner is R else t.half()):
+                with pytest.raises(TypeError, match=name):
+                    setattr(owner, name, bad)
+                assert getattr(owner, name) is t
+    monkeypatch.setattr(torch.Tensor, "is_cuda", False)
+    with pytest.raises(TypeError, match="codes"):
+        R.codes = good["codes"].clone()
+    with pytest.raises(TypeError, match="gate"):
+        L.gate = block["gate"].clone()
+    L.gate = None
+    F = H.FfnLayer.__new__(H.FfnLayer)
+    F.desc, F.held = B.make_ffn_desc(rows=7, width=64, hidden=10), R
+    with pytest.raises(ValueError, match="held"):
+        F.bwd_held()
