@@ -17,9 +17,9 @@ namespace rgnn {
 
 constexpr int UNIT = 32;
 
-template <int D, int PL, bool HELD = false> struct Cut {
+template <int D, int PL> struct Cut {
     static constexpr int MT = PL == 1 && D < 128 ? 32 : 16;      // hidden values of a wavefront
-    static constexpr int lds = 2 * (x_planes(PL, HELD) + PL) * UNIT * D * 2;        // two units of either tensor
+    static constexpr int lds = 2 * 2 * PL * UNIT * D * 2;        // two units of either tensor (of held rows in fp32 a third is left over)
 };
 struct FfnGradArgs {
     FfnArgs a;
