@@ -12,7 +12,7 @@
 // hidden value.  Against 1160 TFLOP/s of a large bf16 product, in brackets what the matrix instructions do:
 //   forward   2M rows, d 128, f 512, bf16: 1007 us, 781 TFLOP/s (1040); 1M rows, d 64, f 256, bf16: 174 us, 565 (753); fp32: 520 us, 189 (1134)
 //   backward  200017 rows, d 128, f 341, bf16: 311 us, 449 (900); 1M rows, d 64, f 256, bf16: 669 us, 392 (783); fp32: 1901 us, 138 (1138)
-// From rows held in 8 bits, whose values are one bfloat16 plane, four of the eleven products of fp32 take three plane products instead of six, 48 of 66: 1M rows, d 64, f 256, 1391 us for
+// From rows held in 8 bits, whose values are one bfloat16 plane, six of the eleven products of fp32 take three plane products instead of six, 48 of 66 in all: 1M rows, d 64, f 256, 1391 us for
 // 1805, f 170 1041 for 1368; 300000 rows, d 128, f 341, 1480 for 1820.  In bf16 there is nothing to save, and the weights' gradients unpack a unit of rows once for each
 // workgroup of hidden values, a quarter more vector instructions: 200017 rows, d 128, f 341, 320 us for 300.
 #include <math.h>

@@ -503,3 +503,63 @@ def test_many_types_of_wide_rows(rows, width, types, order, pad, dtypes):
         torch.cuda.synchronize()
         for n, w in zip(ALL, want):
             assert torch.equal(getattr(L, n), w), n
+
+
+@pytest.mark.parametrize("rows,width,dtypes,types", [(1000000, 64, ("f32", "f32", "bf16"), 4), (700001, 100, ("bf16", "bf16", "f32"), 3), (600000, 349, ("bf16", "bf16", "bf16"), 2)])
+def test_results_past_the_caches(rows, width, dtypes, types):
+    """Results larger than the caches with mixed types of tensors, several types of rows and padding, from the rows themselves: the bits of the first and last
+    rows by themselves, zeros for the rows of zeros between them and for the padding."""
+    import torch
+    k = 400
+    print(f"block_norm case rows={rows} width={width} types={types} {dtypes}, past the caches", flush=True)
+    d = inputs(2 * k, width, types, "sorted", 30, *dtypes, 23)
+    small = layer(d, types, *dtypes)
+    small.fwd()
+    small.bwd()
+    from paper_2412_04747_amd.harness import BlockNormLayer
+    L = BlockNormLayer(rows, width, *dtypes, types, EPS)
+    L.w_after, L.w_before, L.gate, L.scale = small.w_after, small.w_before, small.gate, small.scale
+    for name in ("a", "s", "dOut", "dSum", "types"):
+        part = getattr(small, name)
+        t = torch.zeros(rows, *part.shape[1:], device="cuda", dtype=part.dtype)
+        t[:k], t[-k:] = part[:k], part[k:]
+        if name == "types":
+            t[k:-k] = part[k]                            # (in order, as the rows around are)
+        setattr(L, name, t)
+    for name in ("sum", "out", "dA", "dS"):
+        getattr(L, name).fill_(3.0)
+    L.fwd()
+    L.bwd()
+    torch.cuda.synchronize()
+    for name in ("sum", "out", "dA", "dS"):
+        t, w = getattr(L, name), getattr(small, name)
+        assert torch.equal(t[:k], w[:k]) and torch.equal(t[-k:], w[k:]), name
+        assert not t[k:-k].any() and not t[-30:].any(), name
+    r, m = definition(d, types)
+    # (more rows per lane: what is added is zeros, which round nothing)
+    within(L, d, r, m, ("dGate", "dWAfter", "dScale", "dWBefore"))
+
+
+def test_offsets_past_32_bits_from_the_rows_themselves():
+    """2.2e9 elements in bf16, not held: the last rows and the first, with zeros between."""
+    import torch
+    from paper_2412_04747_amd.harness import BlockNormLayer
+    rows, width, k, dtypes = 17200000, 128, 400, ("bf16", "bf16", "bf16")
+    print(f"block_norm case rows={rows} width={width} bf16, large, not held", flush=True)
+    d = inputs(2 * k, width, 1, "sorted", 0, *dtypes, 24)
+    small = layer(d, 1, *dtypes)
+    small.bwd()
+    L = BlockNormLayer(rows, width, *dtypes, 1, EPS)
+    L.w_after, L.w_before, L.gate, L.scale = small.w_after, small.w_before, small.gate, small.scale
+    for name in ("a", "s", "dOut", "dSum"):
+        t = torch.zeros(rows, width, device="cuda", dtype=torch.bfloat16)
+        t[:k], t[-k:] = getattr(small, name)[:k], getattr(small, name)[k:]
+        setattr(L, name, t)
+    L.bwd()
+    torch.cuda.synchronize()
+    for name in ("dA", "dS"):
+        t, w = getattr(L, name), getattr(small, name)
+        assert torch.equal(t[:k], w[:k]) and torch.equal(t[-k:], w[k:]), name
+        assert not t[k:-k].any(), name
+    r, m = definition(d, 1)
+    within(L, d, r, m, ("dGate", "dWAfter", "dScale", "dWBefore"))
