@@ -3,7 +3,9 @@
 // Twelve operations per element against 8 to 16 bytes: the memory's rate is the bound.  A row's a and s stay in the registers of the lanes that loaded them from
 // the first norm's sum to the second's, so that each tensor is passed once, where the two norms and the gate by themselves pass n and the sum again.
 // The same registers are packed to 8 bits where the backward is to read them so.  Against 4.9 TB/s of a large copy: 1M rows of 64, fp32 to bf16, four types, 150 us (6.0 TB/s);
-// 2M rows of 128, bf16, 364 (5.6); 200017 rows of 128, fp32, left in 8 bits too, 82 (5.6); one row 2.4.
+// 2M rows of 128, bf16, 364 (5.6); 200017 rows of 128, fp32, left in 8 bits too, 82 (5.6); one row 2.4.  Without norms, gate and scale of four mixed types, 1M rows of 64, fp32, 130 (5.9).
+// Rows of odd widths are further off, with some lanes idle and rows at any address: 30011 of 349, fp32, 39 (4.3), seven mixed types 50 (3.4); bf16, by vectors of four columns too and so
+// with fp32's instructions for half its bytes, 28 and 39 (3.0, 2.1).
 #include <float.h>
 
 #include "rgnn_internal.h"

@@ -7,8 +7,9 @@
 // that type in the LDS, which is its wavefront's (lanes of one wavefront that share columns take turns), so that no order depends on timing.  Nodes are
 // mostly stored type by type: then that is rare.  A workgroup leaves one partial row per type; a second launch adds those in order.
 // Against 4.9 TB/s of a large copy: 1M rows of 64, fp32, four types, 272 us (5.7 TB/s; from 8 bits 212, 5.5; in mixed order 282); 2M rows of 128, bf16, 562 (5.5; from
-// 8 bits 463, 5.6); 30011 rows of 349, fp32, 65 (3.8), seven mixed types 82.  Before the next row's tensors were fetched while a row is worked on, and the
-// addresses had 32 bits of their own, the same kernel took 1000 us for 2M rows of 128 from 8 bits.
+// 8 bits 463, 5.6); 30011 rows of 349, fp32, 65 (3.8), seven mixed types 82; bf16, by vectors of four columns too,
+// 45 and 60 (2.8, 2.1); 100000 from 8 bits, fp32, 185 and 261 (3.4, 2.4).  Without norms, 1M rows of 64, four mixed types, 265 (4.9).  Before the next row's
+// tensors were fetched while a row is worked on, and the addresses had 32 bits of their own, the same kernel took 1000 us for 2M rows of 128 from 8 bits.
 #pragma once
 #include <float.h>
 

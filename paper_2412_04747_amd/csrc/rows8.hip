@@ -3,7 +3,8 @@
 // Five and three operations per value against 5 bytes (fp32) or 3 (bf16): the memory's rate is the bound.  A lane takes 16 bytes of x, and eight lanes
 // (bf16: four) a block of 32 columns, whose largest value they find by lane moves.  Against 5.0 TB/s of a large copy: 2M rows of 128, bf16, packed in 113 us
 // (6.9 TB/s) and unpacked in 116; 1M rows of 64, fp32, 51 and 45; 100003 rows of 349, fp32, 35 and 36, bf16, 26 and 28.  A workgroup for each 512 vectors, two per
-// lane; 8192 workgroups that take several turns of four vectors: 116 and 127 us.
+// lane; 8192 workgroups that take several turns of four vectors: 116 and 127 us.  Rows narrower than a block leave lanes idle, as each takes a whole block's: 2M rows of 9, fp32, 50 and 44 us
+// (1.8 and 2.1 TB/s), bf16 35 and 26 (1.6, 2.1); of 17, fp32, 51 and 54 (3.3, 3.2), bf16 37 and 34 (2.8, 3.0).
 #include "rgnn_internal.h"
 #include "device_utils.h"
 #include "rows8.h"
